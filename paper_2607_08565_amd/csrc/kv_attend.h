@@ -1,0 +1,128 @@
+// The plan of an attention step and what its kernels share.  Not part of the ABI.
+#pragma once
+
+#include "kv_common.h"
+
+namespace smk {
+
+// Rows.  The n new tokens of a request and the G query heads that read one key-value head
+// make n G rows of one matrix product, row = token * G + head: the heads share every key
+// that is loaded.  Rows are cut into tiles, a tile's visible keys into parts:
+//   few rows   16 rows a tile, one workgroup's wavefronts each taking keys of their own
+//              (decoding, drafts): kv_few.hip
+//   many rows  128 rows a tile, the wavefronts each taking rows of their own and sharing
+//              the keys through LDS (prompts' chunks): kv_many.hip
+constexpr int FEW_ROWS = 16, MANY_ROWS = 128;
+constexpr int KEY_STEP = 64;  // parts begin at multiples of this many keys
+inline int32_t rows_per_tile(int32_t n_q, int32_t n_kv, int32_t max_new) {
+  return int64_t(max_new) * (n_q / n_kv) <= FEW_ROWS ? FEW_ROWS : MANY_ROWS;
+}
+
+// One piece of work: the keys [k0, k1) of one tile, for every key-value head.
+struct PlanItem {
+  int32_t req, tok0, n_new, kv_len;  // the request, its first new token, its lengths
+  int32_t tile;
+  int32_t k0, k1;
+  int32_t part;  // slot for a partial result, -1: the tile's only piece, writes the output
+};
+struct PlanSplit {  // a tile of more than one piece
+  int32_t tok0, n_new, tile, part0, n_parts, pad[3];
+};
+struct PlanHdr {
+  int32_t err, n_items, n_splits;
+  int32_t n_req, n_q, n_kv, rows, window;
+  int64_t n_tokens;
+  int32_t pad[22];
+};
+static_assert(sizeof(PlanHdr) == 128 && sizeof(PlanItem) == 32 && sizeof(PlanSplit) == 32, "plan layout");
+
+// Workgroups that the split of a step aims at, over all key-value heads: a tile is cut when
+// its keys are more than its share of them.
+constexpr int32_t FEW_TARGET = 1024, MANY_TARGET = 512;
+constexpr int32_t FEW_MIN_KEYS = 256, MANY_MIN_KEYS = 512;  // no piece of a cut tile is shorter
+
+struct PlanShape {
+  int32_t rows, target;  // rows per tile; pieces aimed at per key-value head
+  int64_t max_tiles, max_items, max_splits, max_parts;
+  uint64_t plan_bytes, ws_bytes;
+  int64_t off_items, off_splits;
+};
+// Tiles: request r's are numbered from floor(q_off[r] G / rows) + r on, which leaves each
+// request room for ceil(n G / rows) and needs no scan.  A tile of u units is cut into
+// ceil(u / c) pieces with c >= total / target, so all tiles together make at most max_tiles +
+// target pieces, at most target tiles have more than one, and those at most 2 target pieces.
+inline PlanShape plan_shape(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t max_new) {
+  PlanShape s;
+  s.rows = rows_per_tile(n_q, n_kv, max_new);
+  s.target = (s.rows == FEW_ROWS ? FEW_TARGET : MANY_TARGET) / n_kv;
+  if (s.target < 1) s.target = 1;
+  s.max_tiles = n_tokens * (n_q / n_kv) / s.rows + n_req;
+  s.max_items = s.max_tiles + s.target;
+  s.max_splits = s.target;
+  s.max_parts = 2 * int64_t(s.target);
+  s.off_items = sizeof(PlanHdr);
+  s.off_splits = s.off_items + s.max_items * int64_t(sizeof(PlanItem));
+  s.plan_bytes = uint64_t(s.off_splits + s.max_splits * int64_t(sizeof(PlanSplit)) + 255) / 256 * 256;
+  // per part, key-value head and row: the sums over its keys, then their maximum and weight
+  s.ws_bytes = uint64_t(s.max_parts) * n_kv * s.rows * (head_dim + 2) * 4;
+  return s;
+}
+
+struct PartView {
+  float *acc;  // [part][kv head][row][head_dim]
+  f32x2 *ml;   // [part][kv head][row]: maximum (in powers of two), sum of weights
+};
+struct AttendArgs {
+  const PlanHdr *hdr;
+  const PlanItem *items;
+  const PlanSplit *splits;
+  CacheView cache;
+  HeadsView q, out;
+  float *lse;
+  PartView parts;
+  int64_t n_tokens;
+  int32_t n_req, n_q, n_kv, group;  // group = n_q / n_kv
+  int32_t rows, window;
+  float scale_log2;  // scale * log2(e)
+  int32_t *status;
+};
+__device__ __forceinline__ bool plan_fits(const AttendArgs &a) {
+  const PlanHdr *h = a.hdr;
+  return h->err == 0 && h->n_req == a.n_req && h->n_q == a.n_q && h->n_kv == a.n_kv && h->rows == a.rows &&
+         h->window == a.window && h->n_tokens == a.n_tokens;
+}
+
+// lse from a row's maximum (in powers of two) and sum of weights.
+template <typename T>
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.0f ? -INFINITY : (m + (log2f(l) - T::P_SHIFT)) * 0.693147180559945309f;
+}
+
+// Launches (one per file).  Grids cover plan_shape's bounds; workgroups past the plan's
+// counts end at once.
+int launch_few(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_items, hipStream_t stream);
+int launch_many(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_items, hipStream_t stream);
+
+// Whether one of eight 16-bit floats is infinite or NaN: its exponent is all ones, and adding
+// the exponent's lowest bit to the exponent alone carries into the (cleared) sign bit.
+template <typename T>
+__device__ __forceinline__ bool any_not_finite(u32x4 x) {
+  uint32_t c = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c |= (x[i] & T::EXP) + T::ONE_EXP;
+  return (c & 0x80008000u) != 0;
+}
+
+// An invalid plan's outputs: zeros and -inf, dealt to all workgroups.
+template <int D>
+__device__ __forceinline__ void write_nothing(const AttendArgs &a) {
+  const int64_t rows = a.n_tokens * a.n_q, step = int64_t(gridDim.x) * blockDim.x;
+  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < rows * (D / 8); i += step) {
+    const int64_t row = i / (D / 8), t = row / a.n_q, h = row - t * a.n_q;
+    *reinterpret_cast<u32x4 *>(a.out.data + t * a.out.token + h * a.out.head + (i % (D / 8)) * 8) = u32x4{0, 0, 0, 0};
+    if (a.lse && i % (D / 8) == 0) a.lse[row] = -INFINITY;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) set_status(a.status, SMETRIC_EINVAL);
+}
+
+}  // namespace smk

@@ -1,0 +1,353 @@
+// Attention of many rows over a paged cache: the chunk of a prompt that is left after its hit.
+//
+// Mathematics (smetric_kv.h): out = sum_j p_j v_j / sum_j p_j with p_j = 2^(c s_j - m), c =
+// scale log2(e), in one pass over the keys: m is the running maximum of c s_j, and what was
+// summed before a larger one appears is scaled down by 2^(old - new).
+//
+// Bound: 4 head_dim operations per row and key that sees it, on the matrix cores; the keys of
+// a tile are read once per 128 rows.  A wavefront holds 32 rows: their queries, their sums
+// (O^T) and one step's scores stay in registers; 64 keys and values at a time go through LDS,
+// where the workgroup's wavefronts share them, double-buffered, the next 64 on their way from
+// memory during the current ones' products.  The products are S^T = K Q^T and O^T = V^T P^T:
+// a lane holds scores of one row only, so its maximum takes one lane exchange, and its weights
+// are where the second product wants them -- the order in which S^T leaves the keys is the
+// order in which V^T is read, transposed, from LDS.
+#include <math.h>
+
+#include "kv_attend.h"
+
+namespace smk {
+namespace {
+
+constexpr int MW = 4;         // wavefronts
+constexpr int MT = 64 * MW;   // threads
+constexpr int KT = KEY_STEP;  // keys of a step
+
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+__device__ __forceinline__ u32x2 read_transposed(const char *lds) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (__attribute__((address_space(3))) s16x4 *)lds));
+}
+__device__ __forceinline__ u32x2 swap32(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
+}
+
+// WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
+template <typename T, bool KV8, int D, bool WIDE>
+__global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a) {
+  constexpr int ESZ = KV8 ? 1 : 2;
+  constexpr int LPR = D * ESZ / 16;   // lanes per row of keys or values
+  constexpr int RPW = 64 / LPR;       // rows of a wavefront's load
+  constexpr int RPL = RPW * MW;       // rows of a workgroup's load
+  constexpr int NL = KT / RPL;        // loads of a lane per step and side
+  constexpr int STEPS = D / 16, DT = D / 32;
+  constexpr int ROWB = 2 * D;         // bytes of a row in LDS
+  constexpr int KSW = D == 64 ? 7 : 15, VSW = D == 64 ? 3 : 7;  // exchange of 16-byte pieces within a row
+  __shared__ __attribute__((aligned(16))) char klds[2][KT * ROWB];
+  __shared__ __attribute__((aligned(16))) char vlds[2][KT * ROWB];
+  __shared__ int32_t odd_step[2];
+
+  if (!plan_fits(a)) {
+    write_nothing<D>(a);
+    return;
+  }
+  const int32_t kvh = blockIdx.x % a.n_kv, at = blockIdx.x / a.n_kv;
+  if (at >= a.hdr->n_items) return;
+  const PlanItem it = a.items[at];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int col = lane & 31, half = lane >> 5;
+  const int32_t row0 = it.tile * MANY_ROWS + 32 * wave;
+  int32_t n_rows = it.n_new * a.group - row0;  // of this wavefront
+  if (n_rows > 32) n_rows = 32;
+  int32_t k0 = it.k0, k1 = it.k1;
+  if (int64_t(it.kv_len) > int64_t(a.cache.max_pages) * a.cache.ps.size) {
+    k0 = k1 = 0;
+    if (threadIdx.x == 0) set_status(a.status, SMETRIC_EINVAL);
+  }
+  if (threadIdx.x < 2) odd_step[threadIdx.x] = -1;
+
+  const bool has_row = col < n_rows;
+  const int32_t row = row0 + col, tok = row / a.group, head = kvh * a.group + row % a.group;
+  const int32_t place = it.kv_len - it.n_new + tok;
+  const int32_t hi = has_row ? place + 1 : 0;
+  const int32_t lo = a.window > 0 ? place - a.window + 1 : 0;
+  // the wavefront's first and last row
+  const int32_t min_hi = it.kv_len - it.n_new + row0 / a.group + 1;
+  const int32_t max_hi = n_rows > 0 ? it.kv_len - it.n_new + (row0 + n_rows - 1) / a.group + 1 : 0;
+  const int32_t min_lo = a.window > 0 ? min_hi - a.window : 0, max_lo = a.window > 0 ? max_hi - a.window : 0;
+  // the tile's: a step that some row does not see whole is watched for values that are not finite
+  const int32_t tile_min_hi = it.kv_len - it.n_new + it.tile * MANY_ROWS / a.group + 1;
+  int32_t tile_end = (it.tile + 1) * MANY_ROWS;
+  if (tile_end > it.n_new * a.group) tile_end = it.n_new * a.group;
+  const int32_t tile_max_lo = a.window > 0 ? it.kv_len - it.n_new + (tile_end - 1) / a.group + 1 - a.window : 0;
+
+  u32x4 q[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    q[s] = u32x4{0, 0, 0, 0};
+    if (has_row)
+      q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + s * 16 +
+                                              half * 8);
+  }
+  const char *kbase = a.cache.k.base + kvh * a.cache.k.head;
+  const char *vbase = a.cache.v.base + kvh * a.cache.v.head;
+  const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
+  const float sc = a.scale_log2 * (KV8 && a.cache.k_scale ? a.cache.k_scale[kvh] : 1.0f);
+
+  bool bad_page = false;
+  const auto page_id = [&](int32_t page) {
+    int32_t id = table[page];
+    if (uint32_t(id) >= uint32_t(a.cache.n_pages)) {
+      id = 0;
+      bad_page = true;
+    }
+    return id;
+  };
+  const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
+  u32x4 kr[NL], vr[NL];
+  int32_t ids = 0, ids_from = 0;  // WIDE: lane l's page of the 16 keys from ids_from + 16 l on
+  const int lrow = lane / LPR, lcol = lane % LPR;
+  const auto load_ids = [&](int32_t kb) {
+    int32_t key = kb + 16 * lane;
+    key = key < last_key ? key : last_key & ~15;
+    key = key > k0 ? key : k0;
+    ids = page_id(page_of(a.cache.ps, key & ~15));
+    ids_from = kb;
+  };
+  const auto load_step = [&](int32_t kb) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = i * RPL + wave * RPW;
+      if (WIDE) {
+        const int32_t id = __builtin_amdgcn_readlane(ids, (kb - ids_from + r) / 16);
+        int32_t g = kb + r / 16 * 16;  // a group outside [k0, k1) reads a neighbour's place: in bounds, not seen
+        g = g < last_key ? g : last_key & ~15;
+        g = g > k0 ? g : k0 & ~15;
+        const int32_t slot = g - page_of(a.cache.ps, g) * a.cache.ps.size + r % 16;
+        const char *kp = kbase + id * a.cache.k.page + slot * a.cache.k.token;
+        const char *vp = vbase + id * a.cache.v.page + slot * a.cache.v.token;
+        kr[i] = *reinterpret_cast<const u32x4 *>(kp + uint32_t(lrow) * uint32_t(a.cache.k.token) + lcol * 16);
+        vr[i] = *reinterpret_cast<const u32x4 *>(vp + uint32_t(lrow) * uint32_t(a.cache.v.token) + lcol * 16);
+      } else {
+        int32_t key = kb + r + lrow;
+        key = key < last_key ? key : last_key;
+        key = key > k0 ? key : k0;
+        const int32_t page = page_of(a.cache.ps, key);
+        const int64_t id = page_id(page), slot = key - page * a.cache.ps.size;
+        kr[i] = *reinterpret_cast<const u32x4 *>(kbase + id * a.cache.k.page + slot * a.cache.k.token + lcol * 16);
+        vr[i] = *reinterpret_cast<const u32x4 *>(vbase + id * a.cache.v.page + slot * a.cache.v.token + lcol * 16);
+      }
+    }
+  };
+  const auto store_step = [&](int32_t kb, int buf) {
+    const bool partial = kb < k0 || kb + KT > k1;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = i * RPL + wave * RPW + lrow;
+      u32x4 k = kr[i], v = vr[i];
+      if (partial && (kb + r < k0 || kb + r >= k1)) v = u32x4{0, 0, 0, 0};
+      char *kp = klds[buf] + r * ROWB, *vp = vlds[buf] + r * ROWB;
+      const int ks = r & KSW, vs = 2 * (r & VSW);
+      if (KV8) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t x = h ? k.z : k.x, y = h ? k.w : k.y, z = h ? v.z : v.x, w = h ? v.w : v.y;
+          const u32x4 k16{T::template from_e4m3<false>(x), T::template from_e4m3<true>(x),
+                          T::template from_e4m3<false>(y), T::template from_e4m3<true>(y)};
+          const u32x4 v16{T::template from_e4m3<false>(z), T::template from_e4m3<true>(z),
+                          T::template from_e4m3<false>(w), T::template from_e4m3<true>(w)};
+          *reinterpret_cast<u32x4 *>(kp + ((2 * lcol + h) ^ ks) * 16) = k16;
+          *reinterpret_cast<u32x4 *>(vp + ((2 * lcol + h) ^ vs) * 16) = v16;
+          odd |= any_not_finite<T>(v16);
+        }
+      } else {
+        *reinterpret_cast<u32x4 *>(kp + (lcol ^ ks) * 16) = k;
+        *reinterpret_cast<u32x4 *>(vp + (lcol ^ vs) * 16) = v;
+      }
+    }
+    if (kb < tile_max_lo || kb + KT > tile_min_hi) {
+      if (!KV8) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int r = i * RPL + wave * RPW + lrow;
+          if (!(partial && (kb + r < k0 || kb + r >= k1))) odd |= any_not_finite<T>(vr[i]);
+        }
+      }
+      if (odd) odd_step[buf] = kb;
+    }
+  };
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+  __syncthreads();  // odd_step is set before a step may mark it
+  if (kb0 < k1) {
+    if (WIDE) load_ids(kb0);
+    load_step(kb0);
+    store_step(kb0, 0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int32_t kb = kb0; kb < k1; kb += KT, buf ^= 1) {
+    const int32_t next = kb + KT;
+    if (next < k1) {
+      if (WIDE && next - ids_from >= 64 * 16) load_ids(next);
+      load_step(next);
+    }
+    if (n_rows > 0 && kb < max_hi && kb + KT > min_lo) {
+      const char *kl = klds[buf], *vl = vlds[buf];
+      // S^T: lane (half, col) gets row col's scores of keys kb + 32 j + 8 (r / 4) + 4 half + r % 4
+      f32x16 s[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) {
+          const int kr_ = 32 * j + col;
+          const u32x4 k = *reinterpret_cast<const u32x4 *>(kl + kr_ * ROWB + (((2 * t + half) ^ (kr_ & KSW)) * 16));
+          s[j] = T::mfma32(k, q[t], s[j]);
+        }
+      }
+      const bool masked = kb < max_lo || kb + KT > min_hi;
+      if (masked) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int32_t key = kb + 32 * j + 8 * (r / 4) + 4 * half + r % 4;
+            if (key >= hi || key < lo) s[j][r] = -INFINITY;
+          }
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[j][r]);
+      const u32x2 both = swap32(__float_as_uint(mx), __float_as_uint(mx));
+      mx = fmaxf(__uint_as_float(both.x), __uint_as_float(both.y)) * sc;
+      if (__any(mx > m)) {
+        const float mn = fmaxf(m, mx);
+        const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= down;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] *= down;
+      }
+      const float base = T::P_SHIFT - (m == -INFINITY ? 0.0f : m);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[j][r] = __builtin_amdgcn_exp2f(fmaf(s[j][r], sc, base));
+          l += s[j][r];
+        }
+      if (masked && odd_step[buf] == kb) {
+        // some value is not finite and rows differ in what they see: 0 times it must not
+        // reach a row that does not see it.  Rare, so plain sums: weight r of either half.
+#pragma unroll 1
+        for (int r = 0; r < 32; ++r) {
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            const float w = __shfl(s[0][0], col + 32 * h);
+            const int vrow = 32 * (r / 16) + 8 * (r % 16 / 4) + 4 * h + r % 4, key = kb + vrow;
+            const bool seen = key < hi && key >= lo;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {  // components 32 i + 8 g + 4 half + 0 .. 3
+                const u32x2 x = *reinterpret_cast<const u32x2 *>(vl + vrow * ROWB +
+                                                                 (((4 * i + g) ^ (2 * (vrow & VSW))) * 16) + half * 8);
+                const float v[4] = {T::lo(x.x), T::hi(x.x), T::lo(x.y), T::hi(x.y)};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[i][4 * g + k] = seen ? fmaf(w, v[k], o[i][4 * g + k]) : o[i][4 * g + k];
+              }
+          }
+#pragma unroll
+          for (int k = 0; k < 31; ++k) s[k / 16][k % 16] = s[(k + 1) / 16][(k + 1) % 16];
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < KT / 16; ++t) {
+          u32x4 p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = T::pack(s[t / 2][8 * (t % 2) + 2 * e], s[t / 2][8 * (t % 2) + 2 * e + 1]);
+#pragma unroll
+          for (int i = 0; i < DT; ++i) {
+            const int j = lane & 15;
+            const int r = 16 * t + 4 * half + j / 4, c = 4 * i + 2 * ((lane >> 4) & 1) + (j % 4) / 2;
+            const u32x2 v0 = read_transposed(vl + r * ROWB + ((c ^ (2 * (r & VSW))) * 16) + (j & 1) * 8);
+            const u32x2 v1 = read_transposed(vl + (r + 8) * ROWB + ((c ^ (2 * ((r + 8) & VSW))) * 16) + (j & 1) * 8);
+            o[i] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p, o[i]);
+          }
+        }
+      }
+    }
+    if (next < k1) store_step(next, buf ^ 1);
+    __syncthreads();
+  }
+  if (bad_page) set_status(a.status, SMETRIC_EINVAL);
+  {
+    const u32x2 both = swap32(__float_as_uint(l), __float_as_uint(l));
+    l = __uint_as_float(both.x) + __uint_as_float(both.y);
+  }
+  const float vs = KV8 && a.cache.v_scale ? a.cache.v_scale[kvh] : 1.0f;
+  if (it.part < 0) {
+    const float inv = l == 0.0f ? 0.0f : vs / l;
+    uint16_t *p = a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; g += 2) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {  // halves trade 4 components: each then has 8 in a row
+          const uint32_t x = T::pack(o[i][4 * g + 2 * e] * inv, o[i][4 * g + 2 * e + 1] * inv);
+          const uint32_t y = T::pack(o[i][4 * g + 4 + 2 * e] * inv, o[i][4 * g + 4 + 2 * e + 1] * inv);
+          const u32x2 z = swap32(x, y);
+          w[e] = z.x;
+          w[2 + e] = z.y;
+        }
+        if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = w;
+      }
+    if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of<T>(m, l);
+  } else if (has_row) {
+    const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + 32 * i + 8 * g + 4 * half) =
+            f32x4{o[i][4 * g] * vs, o[i][4 * g + 1] * vs, o[i][4 * g + 2] * vs, o[i][4 * g + 3] * vs};
+    if (half == 0) a.parts.ml[slot] = f32x2{m, l};
+  }
+}
+
+template <typename T, bool KV8, int D>
+int launch_d(const AttendArgs &a, int64_t max_items, hipStream_t stream) {
+  const dim3 grid(uint32_t(max_items * a.n_kv)), block(MT);
+  if (a.cache.ps.size % 16 == 0)
+    many_kernel<T, KV8, D, true><<<grid, block, 0, stream>>>(a);
+  else
+    many_kernel<T, KV8, D, false><<<grid, block, 0, stream>>>(a);
+  return hip_status(hipGetLastError());
+}
+template <typename T, bool KV8>
+int launch_k(const AttendArgs &a, int32_t d, int64_t max_items, hipStream_t stream) {
+  return d == 64 ? launch_d<T, KV8, 64>(a, max_items, stream)
+                 : d == 128 ? launch_d<T, KV8, 128>(a, max_items, stream) : launch_d<T, KV8, 256>(a, max_items, stream);
+}
+
+}  // namespace
+
+int launch_many(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_items, hipStream_t stream) {
+  if (dtype == SMETRIC_BF16)
+    return kv8 ? launch_k<Bf16, true>(a, head_dim, max_items, stream) : launch_k<Bf16, false>(a, head_dim, max_items, stream);
+  return kv8 ? launch_k<F16, true>(a, head_dim, max_items, stream) : launch_k<F16, false>(a, head_dim, max_items, stream);
+}
+
+}  // namespace smk

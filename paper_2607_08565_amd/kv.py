@@ -1,0 +1,237 @@
+"""The instance's side of a routed request: the paged KV cache and what writes and reads it.
+
+A thin ctypes binding of include/smetric_kv.h.  A step of a model's layer on a batch of
+requests, each with one new token or a chunk of them:
+
+    plan.make(q_off, kv_len)                                    # once per step
+    q = kv.append(cache, table, q_off, kv_len, k, v, q=q, rotary=rotary)  # per layer
+    out = kv.attend(q, cache, table, plan)
+
+Tensors go in by data pointer on torch's current stream; there is no CPU fallback.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import torch
+
+from .smetric import EINVAL, SmetricError, _check, _dev, _lib, _stream
+
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
+
+
+class _Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("k_stride", C.c_int64 * 3),
+                ("v_stride", C.c_int64 * 3), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class _Batch(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("n_req", C.c_int32),
+                ("q_off", C.c_void_p), ("kv_len", C.c_void_p), ("n_tokens", C.c_int64)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("table", C.c_void_p), ("n_pos", C.c_int64),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float)]
+
+
+def _heads(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str) -> _Heads:
+    """An activation [tokens, heads, head_dim]; components contiguous, other strides any."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{name}: expected a {dtype} CUDA tensor")
+    if tuple(t.shape) != shape or t.stride(2) != 1:
+        raise ValueError(f"{name}: expected shape {shape} with contiguous components, got {tuple(t.shape)}, "
+                         f"strides {t.stride()}")
+    return _Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _opt(t: torch.Tensor | None, dtype: torch.dtype, name: str):
+    return None if t is None else _dev(t, dtype, name)
+
+
+def _page_table(t: torch.Tensor, n_req: int) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2:
+        raise TypeError("page_table: expected an int32 CUDA matrix")
+    if t.shape[0] != n_req or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"page_table: expected {n_req} rows of contiguous entries, got {tuple(t.shape)}")
+    return t
+
+
+def _batch(page_table: torch.Tensor, q_off: torch.Tensor, kv_len: torch.Tensor, n_tokens: int) -> _Batch:
+    n_req = kv_len.numel()
+    if q_off.numel() != n_req + 1:
+        raise ValueError("q_off: expected one entry more than kv_len")
+    t = _page_table(page_table, n_req)
+    stride = max(t.stride(0), t.shape[1]) if n_req < 2 else t.stride(0)
+    return _Batch(t.data_ptr(), stride, t.shape[1], n_req, _dev(q_off, torch.int64, "q_off"),
+                  _dev(kv_len, torch.int32, "kv_len"), n_tokens)
+
+
+class PagedCache:
+    """Keys and values in pages: two tensors [n_pages, n_kv_heads, page_size, head_dim] of any
+    strides with contiguous components (a view of another order is one), bfloat16, float16
+    or float8_e4m3fn -- then with float32 scales per head: a stored x stands for x * scale."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
+                 v_scale: torch.Tensor | None = None):
+        for t, name in ((k, "k"), (v, "v")):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or t.dim() != 4:
+                raise TypeError(f"{name}: expected a CUDA tensor [pages, heads, page_size, head_dim] of 16 or 8 bits")
+            if t.stride(3) != 1:
+                raise ValueError(f"{name}: components must be contiguous")
+        if k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v differ in shape, type or device")
+        if (k_scale is None) != (v_scale is None):
+            raise ValueError("k_scale and v_scale go together")
+        if k_scale is not None and (k.dtype != torch.float8_e4m3fn or k_scale.numel() != k.shape[1] or
+                                    v_scale.numel() != k.shape[1]):
+            raise ValueError("scales: one per head of a float8_e4m3fn cache")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.dtype = k.dtype
+        self.c = _Cache(k.data_ptr(), v.data_ptr(), self.n_pages, (C.c_int64 * 3)(*k.stride()[:3]),
+                        (C.c_int64 * 3)(*v.stride()[:3]), self.page_size, self.n_kv_heads, self.head_dim,
+                        _DTYPES[k.dtype], _opt(k_scale, torch.float32, "k_scale"),
+                        _opt(v_scale, torch.float32, "v_scale"))
+        self.ref = C.addressof(self.c)
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 16,
+              dtype: torch.dtype = torch.bfloat16, device="cuda", **scales) -> "PagedCache":
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device), **scales)
+
+
+class Rotary:
+    """Norm weights (or None) and the table of angles: float32 [positions, rot_dim], a row the
+    cosines then the sines of a position's rot_dim / 2 angles."""
+
+    def __init__(self, table: torch.Tensor | None = None, rot_dim: int | None = None, interleaved: bool = False,
+                 q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6):
+        rot_dim = (0 if table is None else table.shape[1]) if rot_dim is None else int(rot_dim)
+        if rot_dim and (table is None or table.dim() != 2 or table.shape[1] != rot_dim):
+            raise ValueError(f"table: expected [positions, {rot_dim}]")
+        self.table, self.q_weight, self.k_weight, self.rot_dim = table, q_weight, k_weight, rot_dim
+        w = [None if x is None else _dev(x, x.dtype, n) for x, n in ((q_weight, "q_weight"), (k_weight, "k_weight"))]
+        self.c = _Rotary(w[0], w[1], _opt(table, torch.float32, "table") if rot_dim else None,
+                         table.shape[0] if rot_dim else 0, rot_dim, int(interleaved), eps)
+        self.ref = C.addressof(self.c)
+
+    def check(self, dtype: torch.dtype, head_dim: int):
+        for w, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
+            if w is not None and (w.dtype != dtype or w.numel() != head_dim):
+                raise ValueError(f"{name}: expected {head_dim} values of {dtype}")
+
+
+def _type_of(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.bfloat16, torch.float16) or t.dim() != 3:
+        raise TypeError(f"{name}: expected a bfloat16 or float16 CUDA tensor [tokens, heads, head_dim]")
+    return _DTYPES[t.dtype]
+
+
+def _new(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def qk_rotate(q: torch.Tensor, k: torch.Tensor, rotary: Rotary, positions: torch.Tensor | None = None,
+              q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, status: torch.Tensor | None = None):
+    """smetric_qk_rotate: queries and keys [tokens, heads, head_dim] normed and rotated to
+    their positions (int32).  Outputs may be the inputs.  Returns (q_out, k_out)."""
+    dtype = _type_of(q, "q")
+    T, _, D = q.shape
+    rotary.check(q.dtype, D)
+    q_out = _new(q) if q_out is None else q_out
+    k_out = _new(k) if k_out is None else k_out
+    if positions is not None and positions.numel() != T:
+        raise ValueError("positions: expected one per token")
+    a, b = _heads(q, q.dtype, tuple(q.shape), "q"), _heads(q_out, q.dtype, tuple(q.shape), "q_out")
+    c, d = _heads(k, q.dtype, (T, k.shape[1], D), "k"), _heads(k_out, q.dtype, (T, k.shape[1], D), "k_out")
+    _check("smetric_qk_rotate", _lib.smetric_qk_rotate(
+        dtype, D, T, rotary.ref, _opt(positions, torch.int32, "positions"), q.shape[1], C.addressof(a), C.addressof(b),
+        k.shape[1], C.addressof(c), C.addressof(d), _opt(status, torch.int32, "status"), _stream()))
+    return q_out, k_out
+
+
+def append(cache: PagedCache, page_table: torch.Tensor, q_off: torch.Tensor, kv_len: torch.Tensor, k: torch.Tensor,
+           v: torch.Tensor, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+           rotary: Rotary | None = None, positions: torch.Tensor | None = None, status: torch.Tensor | None = None):
+    """smetric_kv_append: the new tokens' keys (normed and rotated) and values into the pages;
+    kv_len counts the new tokens already.  With q its queries normed and rotated are
+    returned (q_out, may be q)."""
+    dtype = _type_of(k, "k")
+    T, H, D = k.shape[0], cache.n_kv_heads, cache.head_dim
+    if rotary is not None:
+        rotary.check(k.dtype, D)
+    batch = _batch(page_table, q_off, kv_len, T)
+    a, b = _heads(k, k.dtype, (T, H, D), "k"), _heads(v, k.dtype, (T, H, D), "v")
+    c = d = None
+    if q is not None:
+        q_out = _new(q) if q_out is None else q_out
+        shape = (T, q.shape[1], D)
+        c, d = _heads(q, k.dtype, shape, "q"), _heads(q_out, k.dtype, shape, "q_out")
+    if positions is not None and positions.numel() != T:
+        raise ValueError("positions: expected one per token")
+    _check("smetric_kv_append", _lib.smetric_kv_append(
+        dtype, cache.ref, C.addressof(batch), None if rotary is None else rotary.ref,
+        _opt(positions, torch.int32, "positions"), 0 if q is None else q.shape[1], c and C.addressof(c),
+        d and C.addressof(d), C.addressof(a), C.addressof(b), _opt(status, torch.int32, "status"), _stream()))
+    return q_out if q is not None else None
+
+
+class Plan:
+    """How a step's attention is split over the GPU: made once per step from the lengths, used
+    by every layer.  The buffers (plan and workspace) are kept; a plan serves any batch of the
+    same n_req and n_tokens after another make()."""
+
+    def __init__(self, n_req: int, n_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_new: int,
+                 window: int = 0, device="cuda", workspace: torch.Tensor | None = None):
+        self.args = (n_req, n_tokens, n_q_heads, n_kv_heads, head_dim, max_new)
+        self.window = int(window)
+        a, b = C.c_uint64(), C.c_uint64()
+        _check("smetric_attend_plan_bytes", _lib.smetric_attend_plan_bytes(*self.args, C.byref(a), C.byref(b)))
+        self.plan_bytes, self.ws_bytes = int(a.value), int(b.value)
+        self.mem = torch.empty(self.plan_bytes, dtype=torch.uint8, device=device)
+        if workspace is not None and workspace.numel() < self.ws_bytes:
+            raise SmetricError("smetric_attend_plan_bytes", EINVAL)
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device) if workspace is None else workspace
+        self.q_off = self.kv_len = None
+
+    def make(self, q_off: torch.Tensor, kv_len: torch.Tensor, status: torch.Tensor | None = None) -> "Plan":
+        """smetric_attend_plan for these lengths (device tensors, read on the current stream)."""
+        n_req, n_tokens = self.args[:2]
+        if kv_len.numel() != n_req or q_off.numel() != n_req + 1:
+            raise ValueError(f"expected {n_req} requests")
+        self.q_off, self.kv_len = q_off, kv_len
+        _check("smetric_attend_plan", _lib.smetric_attend_plan(
+            _dev(q_off, torch.int64, "q_off"), _dev(kv_len, torch.int32, "kv_len"), *self.args, self.window,
+            self.mem.data_ptr(), self.plan_bytes, _opt(status, torch.int32, "status"), _stream()))
+        return self
+
+
+def attend(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, plan: Plan, scale: float | None = None,
+           out: torch.Tensor | None = None, lse: torch.Tensor | None = None, status: torch.Tensor | None = None):
+    """smetric_attend: the new tokens' attention over the pages, as `plan` (made for the batch)
+    splits it.  scale: 1 / sqrt(head_dim) by default; lse (float32 [tokens, heads]) is
+    filled if given.  Returns out [tokens, heads, head_dim]."""
+    dtype = _type_of(q, "q")
+    if plan.kv_len is None:
+        raise ValueError("plan: make() it for the batch first")
+    n_req, T, Hq, H, D, max_new = plan.args
+    if H != cache.n_kv_heads or D != cache.head_dim:
+        raise ValueError("plan and cache differ in heads or head_dim")
+    batch = _batch(page_table, plan.q_off, plan.kv_len, T)
+    out = _new(q) if out is None else out
+    if lse is not None and tuple(lse.shape) != (T, Hq):
+        raise ValueError(f"lse: expected shape {(T, Hq)}")
+    a, b = _heads(q, q.dtype, (T, Hq, D), "q"), _heads(out, q.dtype, (T, Hq, D), "out")
+    _check("smetric_attend", _lib.smetric_attend(
+        dtype, cache.ref, C.addressof(batch), Hq, C.addressof(a), C.addressof(b), _opt(lse, torch.float32, "lse"),
+        1.0 / math.sqrt(D) if scale is None else scale, max_new, plan.window, plan.mem.data_ptr(), plan.plan_bytes,
+        plan.workspace.data_ptr(), plan.ws_bytes, _opt(status, torch.int32, "status"), _stream()))
+    return out

@@ -87,6 +87,12 @@ def _load() -> C.CDLL:
         "smetric_match_probed": [PIX, P, U64, P, P, I32, I64, P, P],
         "smetric_index_insert_probed": [PIX, P, U64, I32, I64, P, P, U32, P, U64, P],
         "smetric_route_score": [I32, P, I32, I32, P, P, P, I32, I32, I32, U64, P, P, P],
+        # the instance's side (smetric_kv.h; marshalled by kv.py)
+        "smetric_qk_rotate": [I32, I32, I64, P, P, I32, P, P, I32, P, P, P, P],
+        "smetric_kv_append": [I32, P, P, P, P, I32, P, P, P, P, P, P],
+        "smetric_attend_plan_bytes": [I32, I64, I32, I32, I32, I32, P, P],
+        "smetric_attend_plan": [P, P, I32, I64, I32, I32, I32, I32, I32, P, U64, P, P],
+        "smetric_attend": [I32, P, P, I32, P, P, P, C.c_float, I32, I32, P, U64, P, U64, P, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -107,6 +113,7 @@ EXPORTED = (
     "smetric_probe_partition", "smetric_probe_lookup", "smetric_hash_partition", "smetric_route_seq_coloc",
     "smetric_route_seq_coloc_ws_bytes", "smetric_route_seq_noalloc", "smetric_route_seq_noalloc_max_req",
     "smetric_probe_stats", "smetric_route_score",
+    "smetric_qk_rotate", "smetric_kv_append", "smetric_attend_plan_bytes", "smetric_attend_plan", "smetric_attend",
 )
 
 
