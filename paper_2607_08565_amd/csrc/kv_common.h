@@ -26,7 +26,7 @@ constexpr float E4M3_MAX = 448.0f;
 struct Bf16 {
   typedef bf16x8 V8;
   static constexpr uint32_t EXP = 0x7F807F80u, ONE_EXP = 0x00800080u;  // exponent bits, their lowest (both halves)
-  static constexpr float P_SHIFT = 0.0f;  // see the attention kernels
+  static constexpr float P_SHIFT = 0.0f;  // weights are held times 2^P_SHIFT
   __device__ static __forceinline__ float lo(uint32_t x) { return __uint_as_float(x << 16); }
   __device__ static __forceinline__ float hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
   __device__ static __forceinline__ uint32_t pack(float a, float b) {  // to nearest even, v_cvt_pk_bf16_f32
@@ -47,7 +47,7 @@ struct Bf16 {
 struct F16 {
   typedef f16x8 V8;
   static constexpr uint32_t EXP = 0x7C007C00u, ONE_EXP = 0x04000400u;
-  static constexpr float P_SHIFT = 8.0f;
+  static constexpr float P_SHIFT = 4.0f;
   __device__ static __forceinline__ float lo(uint32_t x) { return float(__builtin_bit_cast(f16x2, x).x); }
   __device__ static __forceinline__ float hi(uint32_t x) { return float(__builtin_bit_cast(f16x2, x).y); }
   __device__ static __forceinline__ uint32_t pack(float a, float b) {

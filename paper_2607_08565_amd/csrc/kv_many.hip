@@ -8,7 +8,7 @@
 // a tile are read once per 128 rows.  A wavefront holds 32 rows: their queries, their sums
 // (O^T) and one step's scores stay in registers; 64 keys and values at a time go through LDS,
 // where the workgroup's wavefronts share them, double-buffered, the next 64 on their way from
-// memory during the current ones' products.  The products are S^T = K Q^T and O^T = V^T P^T:
+// memory (16-bit ones straight to LDS, past the registers) during the current ones' products.  The products are S^T = K Q^T and O^T = V^T P^T:
 // a lane holds scores of one row only, so its maximum takes one lane exchange, and its weights
 // are where the second product wants them -- the order in which S^T leaves the keys is the
 // order in which V^T is read, transposed, from LDS.
@@ -32,6 +32,129 @@ __device__ __forceinline__ u32x2 swap32(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
 }
 
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+// 64 lanes' 16 bytes from memory to 1 KB of LDS, past the registers.
+__device__ __forceinline__ void to_lds(const char *from, char *to) {
+  __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {  // one instruction; NaN stays
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
+// A row is scaled down only when its maximum has grown by more than 2^SLACK: until then its
+// weights are at most 2^SLACK instead of 1, which costs no precision, and most steps of a
+// long request leave the sums alone.
+constexpr float SLACK = 8.0f;
+
+// What a wavefront keeps of its 32 rows; lane (half, col) holds row col's.
+template <int D>
+struct Rows {
+  u32x4 q[D / 16];
+  f32x16 o[D / 32];  // O^T: components 32 i + 8 (r / 4) + 4 half + r % 4
+  float m, l;        // of the half's keys (l), of all (m)
+  int32_t hi, lo;    // the keys [lo, hi) that the row sees
+};
+
+// One step's 64 keys.  MASKED: some row does not see all of them; odd: and some value is not
+// finite.
+template <typename T, int D, bool MASKED>
+__device__ __forceinline__ void step(Rows<D> &w, const char (&kl)[KT * 2 * D], const char (&vl)[KT * 2 * D], int32_t kb,
+                                     float sc, bool odd, int lane) {
+  constexpr int STEPS = D / 16, DT = D / 32, ROWB = 2 * D;
+  constexpr int KSW = D == 64 ? 7 : 15, VSW = D == 64 ? 3 : 7;
+  const int col = lane & 31, half = lane >> 5;
+  // S^T: lane (half, col) gets row col's scores of keys kb + 32 j + 8 (r / 4) + 4 half + r % 4
+  f32x16 s[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) {
+      const int kr = 32 * j + col;
+      const u32x4 k = *reinterpret_cast<const u32x4 *>(kl + kr * ROWB + (((2 * t + half) ^ (kr & KSW)) * 16));
+      s[j] = T::mfma32(k, w.q[t], s[j]);
+    }
+  }
+  if (MASKED) {
+    const int32_t hi = w.hi - kb - 4 * half, lo = w.lo - kb - 4 * half;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int32_t key = 32 * j + 8 * (r / 4) + r % 4;
+        if (key >= hi || key < lo) s[j][r] = -INFINITY;
+      }
+  }
+  float mx = max3(s[0][0], s[0][1], s[1][0]);
+#pragma unroll
+  for (int r = 2; r < 16; r += 2) mx = max3(mx, s[0][r], s[0][r + 1]);
+#pragma unroll
+  for (int r = 1; r < 15; r += 2) mx = max3(mx, s[1][r], s[1][r + 1]);
+  mx = __builtin_elementwise_maximum(mx, s[1][15]);
+  const u32x2 both = swap32(__float_as_uint(mx), __float_as_uint(mx));
+  mx = __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * sc;
+  if (__any(mx > w.m + SLACK)) {  // also the first one: m is -inf
+    const float mn = fmaxf(w.m, mx);
+    const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
+    w.m = mn;
+    w.l *= down;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) w.o[i] *= down;
+  }
+  const float base = T::P_SHIFT - (w.m == -INFINITY ? 0.0f : w.m);
+  float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], sc, base));
+    s[1][r] = __builtin_amdgcn_exp2f(fmaf(s[1][r], sc, base));
+    l0 += s[0][r];
+    l1 += s[1][r];
+  }
+  w.l += l0 + l1;
+  if (MASKED && odd) {
+    // some value is not finite and rows differ in what they see: 0 times it must not reach a
+    // row that does not see it.  Rare, so plain sums: weight r of either half.
+#pragma unroll 1
+    for (int r = 0; r < 32; ++r) {
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        const float p = __shfl(s[0][0], col + 32 * h);
+        const int vrow = 32 * (r / 16) + 8 * (r % 16 / 4) + 4 * h + r % 4, key = kb + vrow;
+        const bool seen = key < w.hi && key >= w.lo;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {  // components 32 i + 8 g + 4 half + 0 .. 3
+            const u32x2 x = *reinterpret_cast<const u32x2 *>(vl + vrow * ROWB + (((4 * i + g) ^ (2 * (vrow & VSW))) * 16) +
+                                                             half * 8);
+            const float v[4] = {T::lo(x.x), T::hi(x.x), T::lo(x.y), T::hi(x.y)};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w.o[i][4 * g + k] = seen ? fmaf(p, v[k], w.o[i][4 * g + k]) : w.o[i][4 * g + k];
+          }
+      }
+#pragma unroll
+      for (int k = 0; k < 31; ++k) s[k / 16][k % 16] = s[(k + 1) / 16][(k + 1) % 16];
+    }
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < KT / 16; ++t) {
+    u32x4 p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = T::pack(s[t / 2][8 * (t % 2) + 2 * e], s[t / 2][8 * (t % 2) + 2 * e + 1]);
+#pragma unroll
+    for (int i = 0; i < DT; ++i) {
+      const int j = lane & 15;
+      const int r = 16 * t + 4 * half + j / 4, c = 4 * i + 2 * ((lane >> 4) & 1) + (j % 4) / 2;
+      const u32x2 v0 = read_transposed(vl + r * ROWB + ((c ^ (2 * (r & VSW))) * 16) + (j & 1) * 8);
+      const u32x2 v1 = read_transposed(vl + (r + 8) * ROWB + ((c ^ (2 * ((r + 8) & VSW))) * 16) + (j & 1) * 8);
+      w.o[i] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p, w.o[i]);
+    }
+  }
+}
+
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
 template <typename T, bool KV8, int D, bool WIDE>
 __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a) {
@@ -43,9 +166,12 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
   constexpr int STEPS = D / 16, DT = D / 32;
   constexpr int ROWB = 2 * D;         // bytes of a row in LDS
   constexpr int KSW = D == 64 ? 7 : 15, VSW = D == 64 ? 3 : 7;  // exchange of 16-byte pieces within a row
-  __shared__ __attribute__((aligned(16))) char klds[2][KT * ROWB];
-  __shared__ __attribute__((aligned(16))) char vlds[2][KT * ROWB];
-  __shared__ int32_t odd_step[2];
+  // four arrays, so that the compiler sees that loads into one do not change the others
+  __shared__ __attribute__((aligned(1024))) char k_even[KT * ROWB];
+  __shared__ __attribute__((aligned(1024))) char k_odd[KT * ROWB];
+  __shared__ __attribute__((aligned(1024))) char v_even[KT * ROWB];
+  __shared__ __attribute__((aligned(1024))) char v_odd[KT * ROWB];
+  __shared__ int32_t odd_step;  // the last step with a value that is not finite
 
   if (!plan_fits(a)) {
     write_nothing<D>(a);
@@ -64,31 +190,36 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
     k0 = k1 = 0;
     if (threadIdx.x == 0) set_status(a.status, SMETRIC_EINVAL);
   }
-  if (threadIdx.x < 2) odd_step[threadIdx.x] = -1;
+  if (threadIdx.x == 0) odd_step = -1;
 
+  Rows<D> w;
   const bool has_row = col < n_rows;
   const int32_t row = row0 + col, tok = row / a.group, head = kvh * a.group + row % a.group;
-  const int32_t place = it.kv_len - it.n_new + tok;
-  const int32_t hi = has_row ? place + 1 : 0;
-  const int32_t lo = a.window > 0 ? place - a.window + 1 : 0;
-  // the wavefront's first and last row
-  const int32_t min_hi = it.kv_len - it.n_new + row0 / a.group + 1;
-  const int32_t max_hi = n_rows > 0 ? it.kv_len - it.n_new + (row0 + n_rows - 1) / a.group + 1 : 0;
+  const int32_t first = it.kv_len - it.n_new;  // the first new token's place
+  w.hi = has_row ? first + tok + 1 : 0;
+  w.lo = a.window > 0 ? first + tok + 1 - a.window : 0;
+  // the wavefront's first and last row, and the tile's
+  const int32_t min_hi = first + row0 / a.group + 1;
+  const int32_t max_hi = n_rows > 0 ? first + (row0 + n_rows - 1) / a.group + 1 : 0;
   const int32_t min_lo = a.window > 0 ? min_hi - a.window : 0, max_lo = a.window > 0 ? max_hi - a.window : 0;
-  // the tile's: a step that some row does not see whole is watched for values that are not finite
-  const int32_t tile_min_hi = it.kv_len - it.n_new + it.tile * MANY_ROWS / a.group + 1;
+  const int32_t tile_min_hi = first + it.tile * MANY_ROWS / a.group + 1;
   int32_t tile_end = (it.tile + 1) * MANY_ROWS;
   if (tile_end > it.n_new * a.group) tile_end = it.n_new * a.group;
-  const int32_t tile_max_lo = a.window > 0 ? it.kv_len - it.n_new + (tile_end - 1) / a.group + 1 - a.window : 0;
+  const int32_t tile_max_lo = a.window > 0 ? first + (tile_end - 1) / a.group + 1 - a.window : 0;
 
-  u32x4 q[STEPS];
 #pragma unroll
   for (int s = 0; s < STEPS; ++s) {
-    q[s] = u32x4{0, 0, 0, 0};
+    w.q[s] = u32x4{0, 0, 0, 0};
     if (has_row)
-      q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + s * 16 +
-                                              half * 8);
+      w.q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + s * 16 +
+                                                half * 8);
   }
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w.o[i][r] = 0.0f;
+  w.m = -INFINITY;
+  w.l = 0.0f;
   const char *kbase = a.cache.k.base + kvh * a.cache.k.head;
   const char *vbase = a.cache.v.base + kvh * a.cache.v.head;
   const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
@@ -104,7 +235,7 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
     return id;
   };
   const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
-  u32x4 kr[NL], vr[NL];
+  u32x4 kr[KV8 ? NL : 1], vr[KV8 ? NL : 1];  // 8-bit keys and values on their way to LDS
   int32_t ids = 0, ids_from = 0;  // WIDE: lane l's page of the 16 keys from ids_from + 16 l on
   const int lrow = lane / LPR, lcol = lane % LPR;
   const auto load_ids = [&](int32_t kb) {
@@ -114,207 +245,138 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
     ids = page_id(page_of(a.cache.ps, key & ~15));
     ids_from = kb;
   };
-  const auto load_step = [&](int32_t kb) {
+  // From memory: 16-bit rows straight to LDS, each lane fetching the piece that belongs where
+  // its 16 bytes land; 8-bit ones to registers, from which to_16 widens them.
+  const auto load_step = [&](int32_t kb, char *kl, char *vl) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int r = i * RPL + wave * RPW;
+      const int r = i * RPL + wave * RPW;  // the wavefront's first row
+      const int kc = KV8 ? lcol : lcol ^ ((r + lrow) & KSW), vc = KV8 ? lcol : lcol ^ (2 * ((r + lrow) & VSW));
+      const char *kp, *vp;
+      uint32_t ko, vo;
       if (WIDE) {
         const int32_t id = __builtin_amdgcn_readlane(ids, (kb - ids_from + r) / 16);
         int32_t g = kb + r / 16 * 16;  // a group outside [k0, k1) reads a neighbour's place: in bounds, not seen
         g = g < last_key ? g : last_key & ~15;
         g = g > k0 ? g : k0 & ~15;
         const int32_t slot = g - page_of(a.cache.ps, g) * a.cache.ps.size + r % 16;
-        const char *kp = kbase + id * a.cache.k.page + slot * a.cache.k.token;
-        const char *vp = vbase + id * a.cache.v.page + slot * a.cache.v.token;
-        kr[i] = *reinterpret_cast<const u32x4 *>(kp + uint32_t(lrow) * uint32_t(a.cache.k.token) + lcol * 16);
-        vr[i] = *reinterpret_cast<const u32x4 *>(vp + uint32_t(lrow) * uint32_t(a.cache.v.token) + lcol * 16);
+        kp = kbase + id * a.cache.k.page + slot * a.cache.k.token;
+        vp = vbase + id * a.cache.v.page + slot * a.cache.v.token;
+        ko = uint32_t(lrow) * uint32_t(a.cache.k.token) + kc * 16;
+        vo = uint32_t(lrow) * uint32_t(a.cache.v.token) + vc * 16;
       } else {
         int32_t key = kb + r + lrow;
         key = key < last_key ? key : last_key;
         key = key > k0 ? key : k0;
         const int32_t page = page_of(a.cache.ps, key);
         const int64_t id = page_id(page), slot = key - page * a.cache.ps.size;
-        kr[i] = *reinterpret_cast<const u32x4 *>(kbase + id * a.cache.k.page + slot * a.cache.k.token + lcol * 16);
-        vr[i] = *reinterpret_cast<const u32x4 *>(vbase + id * a.cache.v.page + slot * a.cache.v.token + lcol * 16);
+        kp = kbase + id * a.cache.k.page + slot * a.cache.k.token;
+        vp = vbase + id * a.cache.v.page + slot * a.cache.v.token;
+        ko = kc * 16;
+        vo = vc * 16;
+      }
+      if (KV8) {
+        kr[i] = *reinterpret_cast<const u32x4 *>(kp + ko);
+        vr[i] = *reinterpret_cast<const u32x4 *>(vp + vo);
+      } else {
+        to_lds(kp + ko, kl + r * ROWB);
+        to_lds(vp + vo, vl + r * ROWB);
       }
     }
   };
-  const auto store_step = [&](int32_t kb, int buf) {
-    const bool partial = kb < k0 || kb + KT > k1;
-    bool odd = false;
+  const auto to_16 = [&](char *kl, char *vl) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int r = i * RPL + wave * RPW + lrow;
-      u32x4 k = kr[i], v = vr[i];
-      if (partial && (kb + r < k0 || kb + r >= k1)) v = u32x4{0, 0, 0, 0};
-      char *kp = klds[buf] + r * ROWB, *vp = vlds[buf] + r * ROWB;
-      const int ks = r & KSW, vs = 2 * (r & VSW);
-      if (KV8) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t x = h ? k.z : k.x, y = h ? k.w : k.y, z = h ? v.z : v.x, w = h ? v.w : v.y;
-          const u32x4 k16{T::template from_e4m3<false>(x), T::template from_e4m3<true>(x),
-                          T::template from_e4m3<false>(y), T::template from_e4m3<true>(y)};
-          const u32x4 v16{T::template from_e4m3<false>(z), T::template from_e4m3<true>(z),
-                          T::template from_e4m3<false>(w), T::template from_e4m3<true>(w)};
-          *reinterpret_cast<u32x4 *>(kp + ((2 * lcol + h) ^ ks) * 16) = k16;
-          *reinterpret_cast<u32x4 *>(vp + ((2 * lcol + h) ^ vs) * 16) = v16;
-          odd |= any_not_finite<T>(v16);
-        }
-      } else {
-        *reinterpret_cast<u32x4 *>(kp + (lcol ^ ks) * 16) = k;
-        *reinterpret_cast<u32x4 *>(vp + (lcol ^ vs) * 16) = v;
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 k = kr[i], v = vr[i];
+        const uint32_t x = h ? k.z : k.x, y = h ? k.w : k.y, z = h ? v.z : v.x, u = h ? v.w : v.y;
+        *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((2 * lcol + h) ^ (r & KSW)) * 16) =
+            u32x4{T::template from_e4m3<false>(x), T::template from_e4m3<true>(x), T::template from_e4m3<false>(y),
+                  T::template from_e4m3<true>(y)};
+        *reinterpret_cast<u32x4 *>(vl + r * ROWB + ((2 * lcol + h) ^ (2 * (r & VSW))) * 16) =
+            u32x4{T::template from_e4m3<false>(z), T::template from_e4m3<true>(z), T::template from_e4m3<false>(u),
+                  T::template from_e4m3<true>(u)};
       }
-    }
-    if (kb < tile_max_lo || kb + KT > tile_min_hi) {
-      if (!KV8) {
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          const int r = i * RPL + wave * RPW + lrow;
-          if (!(partial && (kb + r < k0 || kb + r >= k1))) odd |= any_not_finite<T>(vr[i]);
-        }
-      }
-      if (odd) odd_step[buf] = kb;
     }
   };
+  // A step at the ends of what the rows see: values outside [k0, k1), which may be anything,
+  // become zeros; a value that is not finite marks the step.
+  const auto look_over = [&](int32_t kb, char *vl) {
+    constexpr int TPR = MT / KT, BYTES = ROWB / TPR;
+    const int r = threadIdx.x / TPR;
+    char *p = vl + r * ROWB + threadIdx.x % TPR * BYTES;
+    const bool in = kb + r >= k0 && kb + r < k1;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < BYTES; i += 16) {
+      if (in)
+        odd |= any_not_finite<T>(*reinterpret_cast<const u32x4 *>(p + i));
+      else
+        *reinterpret_cast<u32x4 *>(p + i) = u32x4{0, 0, 0, 0};
+    }
+    if (odd) odd_step = kb;
+    __syncthreads();
+  };
+  const auto arrived = [] {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  // one step: the next one's loads, this one's products
+  const auto turn = [&](int32_t kb, char(&kl)[KT * ROWB], char(&vl)[KT * ROWB], char *k_next, char *v_next) {
+    const int32_t next = kb + KT;
+    const bool ends = kb < k0 || kb + KT > k1 || kb < tile_max_lo || kb + KT > tile_min_hi;
+    if (next < k1) {
+      if (WIDE && next - ids_from >= 64 * 16) load_ids(next);
+      load_step(next, k_next, v_next);
+    }
+    if (ends) look_over(kb, vl);
+    if (n_rows > 0 && kb < max_hi && kb + KT > min_lo) {
+      if (kb < max_lo || kb + KT > min_hi)
+        step<T, D, true>(w, kl, vl, kb, sc, odd_step == kb, lane);
+      else
+        step<T, D, false>(w, kl, vl, kb, sc, false, lane);
+    }
+    if (KV8 && next < k1) to_16(k_next, v_next);
+    arrived();
+  };
 
-  f32x16 o[DT];
-#pragma unroll
-  for (int i = 0; i < DT; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
   __syncthreads();  // odd_step is set before a step may mark it
   if (kb0 < k1) {
     if (WIDE) load_ids(kb0);
-    load_step(kb0);
-    store_step(kb0, 0);
-  }
-  __syncthreads();
-  int buf = 0;
-  for (int32_t kb = kb0; kb < k1; kb += KT, buf ^= 1) {
-    const int32_t next = kb + KT;
-    if (next < k1) {
-      if (WIDE && next - ids_from >= 64 * 16) load_ids(next);
-      load_step(next);
+    load_step(kb0, k_even, v_even);
+    if (KV8) to_16(k_even, v_even);
+    arrived();
+    for (int32_t kb = kb0; kb < k1; kb += 2 * KT) {
+      turn(kb, k_even, v_even, k_odd, v_odd);
+      if (kb + KT < k1) turn(kb + KT, k_odd, v_odd, k_even, v_even);
     }
-    if (n_rows > 0 && kb < max_hi && kb + KT > min_lo) {
-      const char *kl = klds[buf], *vl = vlds[buf];
-      // S^T: lane (half, col) gets row col's scores of keys kb + 32 j + 8 (r / 4) + 4 half + r % 4
-      f32x16 s[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
-#pragma unroll
-        for (int t = 0; t < STEPS; ++t) {
-          const int kr_ = 32 * j + col;
-          const u32x4 k = *reinterpret_cast<const u32x4 *>(kl + kr_ * ROWB + (((2 * t + half) ^ (kr_ & KSW)) * 16));
-          s[j] = T::mfma32(k, q[t], s[j]);
-        }
-      }
-      const bool masked = kb < max_lo || kb + KT > min_hi;
-      if (masked) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int32_t key = kb + 32 * j + 8 * (r / 4) + 4 * half + r % 4;
-            if (key >= hi || key < lo) s[j][r] = -INFINITY;
-          }
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[j][r]);
-      const u32x2 both = swap32(__float_as_uint(mx), __float_as_uint(mx));
-      mx = fmaxf(__uint_as_float(both.x), __uint_as_float(both.y)) * sc;
-      if (__any(mx > m)) {
-        const float mn = fmaxf(m, mx);
-        const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= down;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) o[i] *= down;
-      }
-      const float base = T::P_SHIFT - (m == -INFINITY ? 0.0f : m);
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[j][r] = __builtin_amdgcn_exp2f(fmaf(s[j][r], sc, base));
-          l += s[j][r];
-        }
-      if (masked && odd_step[buf] == kb) {
-        // some value is not finite and rows differ in what they see: 0 times it must not
-        // reach a row that does not see it.  Rare, so plain sums: weight r of either half.
-#pragma unroll 1
-        for (int r = 0; r < 32; ++r) {
-#pragma unroll 1
-          for (int h = 0; h < 2; ++h) {
-            const float w = __shfl(s[0][0], col + 32 * h);
-            const int vrow = 32 * (r / 16) + 8 * (r % 16 / 4) + 4 * h + r % 4, key = kb + vrow;
-            const bool seen = key < hi && key >= lo;
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-              for (int g = 0; g < 4; ++g) {  // components 32 i + 8 g + 4 half + 0 .. 3
-                const u32x2 x = *reinterpret_cast<const u32x2 *>(vl + vrow * ROWB +
-                                                                 (((4 * i + g) ^ (2 * (vrow & VSW))) * 16) + half * 8);
-                const float v[4] = {T::lo(x.x), T::hi(x.x), T::lo(x.y), T::hi(x.y)};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o[i][4 * g + k] = seen ? fmaf(w, v[k], o[i][4 * g + k]) : o[i][4 * g + k];
-              }
-          }
-#pragma unroll
-          for (int k = 0; k < 31; ++k) s[k / 16][k % 16] = s[(k + 1) / 16][(k + 1) % 16];
-        }
-      } else {
-#pragma unroll
-        for (int t = 0; t < KT / 16; ++t) {
-          u32x4 p;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = T::pack(s[t / 2][8 * (t % 2) + 2 * e], s[t / 2][8 * (t % 2) + 2 * e + 1]);
-#pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            const int j = lane & 15;
-            const int r = 16 * t + 4 * half + j / 4, c = 4 * i + 2 * ((lane >> 4) & 1) + (j % 4) / 2;
-            const u32x2 v0 = read_transposed(vl + r * ROWB + ((c ^ (2 * (r & VSW))) * 16) + (j & 1) * 8);
-            const u32x2 v1 = read_transposed(vl + (r + 8) * ROWB + ((c ^ (2 * ((r + 8) & VSW))) * 16) + (j & 1) * 8);
-            o[i] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p, o[i]);
-          }
-        }
-      }
-    }
-    if (next < k1) store_step(next, buf ^ 1);
-    __syncthreads();
   }
   if (bad_page) set_status(a.status, SMETRIC_EINVAL);
   {
-    const u32x2 both = swap32(__float_as_uint(l), __float_as_uint(l));
-    l = __uint_as_float(both.x) + __uint_as_float(both.y);
+    const u32x2 both = swap32(__float_as_uint(w.l), __float_as_uint(w.l));
+    w.l = __uint_as_float(both.x) + __uint_as_float(both.y);
   }
   const float vs = KV8 && a.cache.v_scale ? a.cache.v_scale[kvh] : 1.0f;
   if (it.part < 0) {
-    const float inv = l == 0.0f ? 0.0f : vs / l;
+    const float inv = w.l == 0.0f ? 0.0f : vs / w.l;
     uint16_t *p = a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
       for (int g = 0; g < 4; g += 2) {
-        u32x4 w;
+        u32x4 x;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {  // halves trade 4 components: each then has 8 in a row
-          const uint32_t x = T::pack(o[i][4 * g + 2 * e] * inv, o[i][4 * g + 2 * e + 1] * inv);
-          const uint32_t y = T::pack(o[i][4 * g + 4 + 2 * e] * inv, o[i][4 * g + 4 + 2 * e + 1] * inv);
-          const u32x2 z = swap32(x, y);
-          w[e] = z.x;
-          w[2 + e] = z.y;
+          const u32x2 z = swap32(T::pack(w.o[i][4 * g + 2 * e] * inv, w.o[i][4 * g + 2 * e + 1] * inv),
+                                 T::pack(w.o[i][4 * g + 4 + 2 * e] * inv, w.o[i][4 * g + 4 + 2 * e + 1] * inv));
+          x[e] = z.x;
+          x[2 + e] = z.y;
         }
-        if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = w;
+        if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
       }
-    if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of<T>(m, l);
+    if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of<T>(w.m, w.l);
   } else if (has_row) {
     const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
 #pragma unroll
@@ -322,8 +384,8 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + 32 * i + 8 * g + 4 * half) =
-            f32x4{o[i][4 * g] * vs, o[i][4 * g + 1] * vs, o[i][4 * g + 2] * vs, o[i][4 * g + 3] * vs};
-    if (half == 0) a.parts.ml[slot] = f32x2{m, l};
+            f32x4{w.o[i][4 * g] * vs, w.o[i][4 * g + 1] * vs, w.o[i][4 * g + 2] * vs, w.o[i][4 * g + 3] * vs};
+    if (half == 0) a.parts.ml[slot] = f32x2{w.m, w.l};
   }
 }
 
