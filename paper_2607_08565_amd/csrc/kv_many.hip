@@ -14,6 +14,8 @@
 // order in which V^T is read, transposed, from LDS.
 #include <math.h>
 
+#include <type_traits>
+
 #include "kv_attend.h"
 
 namespace smk {
@@ -37,6 +39,10 @@ typedef __attribute__((address_space(1))) const void global_void;
 // 64 lanes' 16 bytes from memory to 1 KB of LDS, past the registers.
 __device__ __forceinline__ void to_lds(const char *from, char *to) {
   __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
+}
+__device__ __forceinline__ uint64_t read_lane(uint64_t x, int lane) {
+  return uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(x), lane))) |
+         uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(x >> 32), lane))) << 32;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {  // one instruction; NaN stays
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
@@ -95,7 +101,7 @@ __device__ __forceinline__ void step(Rows<D> &w, const char (&kl)[KT * 2 * D], c
   mx = __builtin_elementwise_maximum(mx, s[1][15]);
   const u32x2 both = swap32(__float_as_uint(mx), __float_as_uint(mx));
   mx = __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * sc;
-  if (__any(mx > w.m + SLACK)) {  // also the first one: m is -inf
+  while (__any(mx > w.m + SLACK)) {  // at most once, and at first: m is -inf.  A loop, so that the sums stay in place
     const float mn = fmaxf(w.m, mx);
     const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
     w.m = mn;
@@ -201,7 +207,7 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
   // the wavefront's first and last row, and the tile's
   const int32_t min_hi = first + row0 / a.group + 1;
   const int32_t max_hi = n_rows > 0 ? first + (row0 + n_rows - 1) / a.group + 1 : 0;
-  const int32_t min_lo = a.window > 0 ? min_hi - a.window : 0, max_lo = a.window > 0 ? max_hi - a.window : 0;
+  const int32_t min_lo = a.window > 0 ? min_hi - a.window : 0;
   const int32_t tile_min_hi = first + it.tile * MANY_ROWS / a.group + 1;
   int32_t tile_end = (it.tile + 1) * MANY_ROWS;
   if (tile_end > it.n_new * a.group) tile_end = it.n_new * a.group;
@@ -225,26 +231,33 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
   const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
   const float sc = a.scale_log2 * (KV8 && a.cache.k_scale ? a.cache.k_scale[kvh] : 1.0f);
 
+  const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
+  u32x4 kr[KV8 ? NL : 1], vr[KV8 ? NL : 1];  // 8-bit keys and values on their way to LDS
+  const int lrow = lane / LPR, lcol = lane % LPR;
   bool bad_page = false;
-  const auto page_id = [&](int32_t page) {
+  // Where a place's keys and values are; a page outside the cache reads page 0.
+  const auto find = [&](int32_t key, uint64_t &kp, uint64_t &vp) {
+    const int32_t page = page_of(a.cache.ps, key);
     int32_t id = table[page];
     if (uint32_t(id) >= uint32_t(a.cache.n_pages)) {
       id = 0;
       bad_page = true;
     }
-    return id;
+    const int32_t slot = key - page * a.cache.ps.size;
+    kp = reinterpret_cast<uint64_t>(kbase) + id * a.cache.k.page + slot * a.cache.k.token;
+    vp = reinterpret_cast<uint64_t>(vbase) + id * a.cache.v.page + slot * a.cache.v.token;
   };
-  const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
-  u32x4 kr[KV8 ? NL : 1], vr[KV8 ? NL : 1];  // 8-bit keys and values on their way to LDS
-  int32_t ids = 0, ids_from = 0;  // WIDE: lane l's page of the 16 keys from ids_from + 16 l on
-  const int lrow = lane / LPR, lcol = lane % LPR;
-  const auto load_ids = [&](int32_t kb) {
-    int32_t key = kb + 16 * lane;
-    key = key < last_key ? key : last_key & ~15;
+  // WIDE: lane l knows where the 16 keys from known_from + 16 l on are, for 16 steps at a time
+  uint64_t kp_l = 0, vp_l = 0;
+  int32_t known_from = 0;
+  const auto find_steps = [&](int32_t kb) {
+    int32_t key = kb + 16 * lane;  // 16 keys outside [k0, k1) read a neighbour's places: in bounds, not seen
+    key = key < last_key ? key : last_key;
     key = key > k0 ? key : k0;
-    ids = page_id(page_of(a.cache.ps, key & ~15));
-    ids_from = kb;
+    find(key & ~15, kp_l, vp_l);
+    known_from = kb;
   };
+  const uint32_t k_lane = uint32_t(lrow) * uint32_t(a.cache.k.token), v_lane = uint32_t(lrow) * uint32_t(a.cache.v.token);
   // From memory: 16-bit rows straight to LDS, each lane fetching the piece that belongs where
   // its 16 bytes land; 8-bit ones to registers, from which to_16 widens them.
   const auto load_step = [&](int32_t kb, char *kl, char *vl) {
@@ -252,35 +265,27 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
     for (int i = 0; i < NL; ++i) {
       const int r = i * RPL + wave * RPW;  // the wavefront's first row
       const int kc = KV8 ? lcol : lcol ^ ((r + lrow) & KSW), vc = KV8 ? lcol : lcol ^ (2 * ((r + lrow) & VSW));
-      const char *kp, *vp;
-      uint32_t ko, vo;
+      uint64_t kp, vp;
+      uint32_t ko = kc * 16, vo = vc * 16;
       if (WIDE) {
-        const int32_t id = __builtin_amdgcn_readlane(ids, (kb - ids_from + r) / 16);
-        int32_t g = kb + r / 16 * 16;  // a group outside [k0, k1) reads a neighbour's place: in bounds, not seen
-        g = g < last_key ? g : last_key & ~15;
-        g = g > k0 ? g : k0 & ~15;
-        const int32_t slot = g - page_of(a.cache.ps, g) * a.cache.ps.size + r % 16;
-        kp = kbase + id * a.cache.k.page + slot * a.cache.k.token;
-        vp = vbase + id * a.cache.v.page + slot * a.cache.v.token;
-        ko = uint32_t(lrow) * uint32_t(a.cache.k.token) + kc * 16;
-        vo = uint32_t(lrow) * uint32_t(a.cache.v.token) + vc * 16;
+        const int from = (kb - known_from + r) / 16;
+        kp = read_lane(kp_l, from);
+        vp = read_lane(vp_l, from);
+        ko += k_lane + uint32_t(r % 16) * uint32_t(a.cache.k.token);
+        vo += v_lane + uint32_t(r % 16) * uint32_t(a.cache.v.token);
       } else {
         int32_t key = kb + r + lrow;
         key = key < last_key ? key : last_key;
         key = key > k0 ? key : k0;
-        const int32_t page = page_of(a.cache.ps, key);
-        const int64_t id = page_id(page), slot = key - page * a.cache.ps.size;
-        kp = kbase + id * a.cache.k.page + slot * a.cache.k.token;
-        vp = vbase + id * a.cache.v.page + slot * a.cache.v.token;
-        ko = kc * 16;
-        vo = vc * 16;
+        find(key, kp, vp);
       }
+      const char *k = reinterpret_cast<const char *>(kp) + ko, *v = reinterpret_cast<const char *>(vp) + vo;
       if (KV8) {
-        kr[i] = *reinterpret_cast<const u32x4 *>(kp + ko);
-        vr[i] = *reinterpret_cast<const u32x4 *>(vp + vo);
+        kr[i] = *reinterpret_cast<const u32x4 *>(k);
+        vr[i] = *reinterpret_cast<const u32x4 *>(v);
       } else {
-        to_lds(kp + ko, kl + r * ROWB);
-        to_lds(vp + vo, vl + r * ROWB);
+        to_lds(k, kl + r * ROWB);
+        to_lds(v, vl + r * ROWB);
       }
     }
   };
@@ -323,34 +328,39 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  // one step: the next one's loads, this one's products
-  const auto turn = [&](int32_t kb, char(&kl)[KT * ROWB], char(&vl)[KT * ROWB], char *k_next, char *v_next) {
+  // One step: the next one's loads, this one's products.  ENDS: some row of the tile does not
+  // see all of its keys.
+  const auto turn = [&](auto ends, int32_t kb, char(&kl)[KT * ROWB], char(&vl)[KT * ROWB], char *k_next, char *v_next) {
+    constexpr bool ENDS = decltype(ends)::value;
     const int32_t next = kb + KT;
-    const bool ends = kb < k0 || kb + KT > k1 || kb < tile_max_lo || kb + KT > tile_min_hi;
     if (next < k1) {
-      if (WIDE && next - ids_from >= 64 * 16) load_ids(next);
+      if (WIDE && next - known_from >= 64 * 16) find_steps(next);
       load_step(next, k_next, v_next);
     }
-    if (ends) look_over(kb, vl);
-    if (n_rows > 0 && kb < max_hi && kb + KT > min_lo) {
-      if (kb < max_lo || kb + KT > min_hi)
-        step<T, D, true>(w, kl, vl, kb, sc, odd_step == kb, lane);
-      else
-        step<T, D, false>(w, kl, vl, kb, sc, false, lane);
-    }
+    if (ENDS) look_over(kb, vl);
+    if (!ENDS || (kb < max_hi && kb + KT > min_lo)) step<T, D, ENDS>(w, kl, vl, kb, sc, ENDS && odd_step == kb, lane);
     if (KV8 && next < k1) to_16(k_next, v_next);
     arrived();
   };
 
   __syncthreads();  // odd_step is set before a step may mark it
   if (kb0 < k1) {
-    if (WIDE) load_ids(kb0);
+    // steps that every row sees whole; the others, and a lone one beside them, take the other form
+    const int32_t full0 = (max(k0, tile_max_lo) + KT - 1) / KT * KT, full1 = min(k1, tile_min_hi);
+    if (WIDE) find_steps(kb0);
     load_step(kb0, k_even, v_even);
     if (KV8) to_16(k_even, v_even);
     arrived();
-    for (int32_t kb = kb0; kb < k1; kb += 2 * KT) {
-      turn(kb, k_even, v_even, k_odd, v_odd);
-      if (kb + KT < k1) turn(kb + KT, k_odd, v_odd, k_even, v_even);
+    int32_t kb = kb0;
+    while (kb < k1) {
+      for (; kb >= full0 && kb + 2 * KT <= full1; kb += 2 * KT) {
+        turn(std::false_type{}, kb, k_even, v_even, k_odd, v_odd);
+        turn(std::false_type{}, kb + KT, k_odd, v_odd, k_even, v_even);
+      }
+      if (kb < k1) turn(std::true_type{}, kb, k_even, v_even, k_odd, v_odd);
+      kb += KT;
+      if (kb < k1) turn(std::true_type{}, kb, k_odd, v_odd, k_even, v_even);
+      kb += KT;
     }
   }
   if (bad_page) set_status(a.status, SMETRIC_EINVAL);
