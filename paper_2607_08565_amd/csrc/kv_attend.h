@@ -29,40 +29,45 @@ struct PlanSplit {  // a tile of more than one piece
   int32_t tok0, n_new, tile, part0, n_parts, pad[3];
 };
 struct PlanHdr {
-  int32_t err, n_items, n_splits;
-  int32_t n_req, n_q, n_kv, rows, window;
+  int32_t err, n_items, n_splits, n_groups;
+  int32_t n_req, n_q, n_kv, rows, window, pad0;
   int64_t n_tokens;
-  int32_t pad[22];
+  int32_t pad[20];
 };
 static_assert(sizeof(PlanHdr) == 128 && sizeof(PlanItem) == 32 && sizeof(PlanSplit) == 32, "plan layout");
 
-// Workgroups that the split of a step aims at, over all key-value heads: a tile is cut when
-// its keys are more than its share of them.
-constexpr int32_t FEW_TARGET = 1024, MANY_TARGET = 512;
-constexpr int32_t FEW_MIN_KEYS = 256, MANY_MIN_KEYS = 512;  // no piece of a cut tile is shorter
+// Workgroups of a step, over all key-value heads: as many as run at once (two on each of 256
+// compute units), each with an equal share of the key steps in order, so that all end
+// together; a share begins and ends within a tile, which is then in pieces, and may hold
+// several tiles.  Two exceptions: no share is smaller than MIN_STEPS, and a cut this near a
+// tile's end goes to the end (EDGE_STEPS).
+constexpr int32_t TARGET = 512;
+constexpr int32_t FEW_MIN_STEPS = 4, MANY_MIN_STEPS = 8, FEW_EDGE_STEPS = 2, MANY_EDGE_STEPS = 4;
 
 struct PlanShape {
-  int32_t rows, target;  // rows per tile; pieces aimed at per key-value head
-  int64_t max_tiles, max_items, max_splits, max_parts;
+  int32_t rows, target;  // rows per tile; workgroups aimed at per key-value head
+  int64_t max_tiles, max_items, max_groups, max_splits, max_parts;
   uint64_t plan_bytes, ws_bytes;
-  int64_t off_items, off_splits;
+  int64_t off_items, off_splits, off_first;
 };
 // Tiles: request r's are numbered from floor(q_off[r] G / rows) + r on, which leaves each
-// request room for ceil(n G / rows) and needs no scan.  A tile of u units is cut into
-// ceil(u / c) pieces with c >= total / target, so all tiles together make at most max_tiles +
-// target pieces, at most target tiles have more than one, and those at most 2 target pieces.
+// request room for ceil(n G / rows) and needs no scan.  Shares have fewer than `target`
+// inner ends, each of which cuts at most one tile: at most max_tiles + target pieces, target
+// tiles of more than one, 2 target pieces of such tiles.
 inline PlanShape plan_shape(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t max_new) {
   PlanShape s;
   s.rows = rows_per_tile(n_q, n_kv, max_new);
-  s.target = (s.rows == FEW_ROWS ? FEW_TARGET : MANY_TARGET) / n_kv;
+  s.target = TARGET / n_kv;
   if (s.target < 1) s.target = 1;
   s.max_tiles = n_tokens * (n_q / n_kv) / s.rows + n_req;
   s.max_items = s.max_tiles + s.target;
+  s.max_groups = s.max_tiles > s.target ? s.max_tiles : s.target;
   s.max_splits = s.target;
   s.max_parts = 2 * int64_t(s.target);
   s.off_items = sizeof(PlanHdr);
   s.off_splits = s.off_items + s.max_items * int64_t(sizeof(PlanItem));
-  s.plan_bytes = uint64_t(s.off_splits + s.max_splits * int64_t(sizeof(PlanSplit)) + 255) / 256 * 256;
+  s.off_first = s.off_splits + s.max_splits * int64_t(sizeof(PlanSplit));
+  s.plan_bytes = uint64_t(s.off_first + (s.max_groups + 1) * 4 + 255) / 256 * 256;
   // per part, key-value head and row: the sums over its keys, then their maximum and weight
   s.ws_bytes = uint64_t(s.max_parts) * n_kv * s.rows * (head_dim + 2) * 4;
   return s;
@@ -76,6 +81,7 @@ struct AttendArgs {
   const PlanHdr *hdr;
   const PlanItem *items;
   const PlanSplit *splits;
+  const int32_t *first;  // workgroup -> its first piece
   CacheView cache;
   HeadsView q, out;
   float *lse;
@@ -86,10 +92,9 @@ struct AttendArgs {
   float scale_log2;  // scale * log2(e)
   int32_t *status;
 };
-__device__ __forceinline__ bool plan_fits(const AttendArgs &a) {
-  const PlanHdr *h = a.hdr;
-  return h->err == 0 && h->n_req == a.n_req && h->n_q == a.n_q && h->n_kv == a.n_kv && h->rows == a.rows &&
-         h->window == a.window && h->n_tokens == a.n_tokens;
+__device__ __forceinline__ bool plan_fits(const AttendArgs &a, const PlanHdr &h) {
+  return h.err == 0 && h.n_req == a.n_req && h.n_q == a.n_q && h.n_kv == a.n_kv && h.rows == a.rows &&
+         h.window == a.window && h.n_tokens == a.n_tokens;
 }
 
 // lse from a row's maximum (in powers of two) and sum of weights.
@@ -100,8 +105,8 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 
 // Launches (one per file).  Grids cover plan_shape's bounds; workgroups past the plan's
 // counts end at once.
-int launch_few(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_items, hipStream_t stream);
-int launch_many(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_items, hipStream_t stream);
+int launch_few(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+int launch_many(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_groups, hipStream_t stream);
 
 // Whether one of eight 16-bit floats is infinite or NaN: its exponent is all ones, and adding
 // the exponent's lowest bit to the exponent alone carries into the (cleared) sign bit.
@@ -111,6 +116,26 @@ __device__ __forceinline__ bool any_not_finite(u32x4 x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) c |= (x[i] & T::EXP) + T::ONE_EXP;
   return (c & 0x80008000u) != 0;
+}
+
+// 16 lanes read four rows' 16 columns of 16-bit values from LDS, each lane's address a row's
+// (lane / 4) four columns (lane % 4): lane i gets column i of the four rows.
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+__device__ __forceinline__ u32x2 read_transposed(const char *lds) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (__attribute__((address_space(3))) s16x4 *)lds));
+}
+__device__ __forceinline__ uint64_t read_lane(uint64_t x, int lane) {
+  return uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(x), lane))) |
+         uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(x >> 32), lane))) << 32;
+}
+
+// A piece, in scalar registers: the compiler cannot know that a load through a pointer that
+// it also sees stores beside is the same for all lanes.
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ PlanItem uniform(const PlanItem &p) {
+  return PlanItem{uniform(p.req),  uniform(p.tok0), uniform(p.n_new), uniform(p.kv_len),
+                  uniform(p.tile), uniform(p.k0),   uniform(p.k1),    uniform(p.part)};
 }
 
 // An invalid plan's outputs: zeros and -inf, dealt to all workgroups.

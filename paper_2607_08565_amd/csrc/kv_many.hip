@@ -25,11 +25,6 @@ constexpr int MW = 4;         // wavefronts
 constexpr int MT = 64 * MW;   // threads
 constexpr int KT = KEY_STEP;  // keys of a step
 
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-__device__ __forceinline__ u32x2 read_transposed(const char *lds) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                       (__attribute__((address_space(3))) s16x4 *)lds));
-}
 __device__ __forceinline__ u32x2 swap32(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
 }
@@ -39,10 +34,6 @@ typedef __attribute__((address_space(1))) const void global_void;
 // 64 lanes' 16 bytes from memory to 1 KB of LDS, past the registers.
 __device__ __forceinline__ void to_lds(const char *from, char *to) {
   __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
-}
-__device__ __forceinline__ uint64_t read_lane(uint64_t x, int lane) {
-  return uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(x), lane))) |
-         uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(x >> 32), lane))) << 32;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {  // one instruction; NaN stays
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
@@ -179,229 +170,233 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
   __shared__ __attribute__((aligned(1024))) char v_odd[KT * ROWB];
   __shared__ int32_t odd_step;  // the last step with a value that is not finite
 
-  if (!plan_fits(a)) {
+  const int32_t kvh = blockIdx.x % a.n_kv, share = blockIdx.x / a.n_kv;
+  // asked for together: a workgroup's start is a chain of round trips
+  const PlanHdr hdr = *a.hdr;
+  const int32_t first_piece = uniform(a.first[share]), last_piece = uniform(a.first[share + 1]);
+  if (!plan_fits(a, hdr)) {
     write_nothing<D>(a);
     return;
   }
-  const int32_t kvh = blockIdx.x % a.n_kv, at = blockIdx.x / a.n_kv;
-  if (at >= a.hdr->n_items) return;
-  const PlanItem it = a.items[at];
+  if (share >= hdr.n_groups) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int col = lane & 31, half = lane >> 5;
-  const int32_t row0 = it.tile * MANY_ROWS + 32 * wave;
-  int32_t n_rows = it.n_new * a.group - row0;  // of this wavefront
-  if (n_rows > 32) n_rows = 32;
-  int32_t k0 = it.k0, k1 = it.k1;
-  if (int64_t(it.kv_len) > int64_t(a.cache.max_pages) * a.cache.ps.size) {
-    k0 = k1 = 0;
-    if (threadIdx.x == 0) set_status(a.status, SMETRIC_EINVAL);
-  }
-  if (threadIdx.x == 0) odd_step = -1;
+  for (int32_t piece = first_piece; piece < last_piece; ++piece) {
+    const PlanItem it = uniform(a.items[piece]);
+    const int32_t row0 = it.tile * MANY_ROWS + 32 * wave;
+    int32_t n_rows = it.n_new * a.group - row0;  // of this wavefront
+    if (n_rows > 32) n_rows = 32;
+    const bool too_long = int64_t(it.kv_len) > int64_t(a.cache.max_pages) * a.cache.ps.size;
+    const int32_t k0 = uniform(too_long ? 0 : it.k0), k1 = uniform(too_long ? 0 : it.k1);
+    if (too_long && threadIdx.x == 0) set_status(a.status, SMETRIC_EINVAL);
+    if (threadIdx.x == 0) odd_step = -1;
 
-  Rows<D> w;
-  const bool has_row = col < n_rows;
-  const int32_t row = row0 + col, tok = row / a.group, head = kvh * a.group + row % a.group;
-  const int32_t first = it.kv_len - it.n_new;  // the first new token's place
-  w.hi = has_row ? first + tok + 1 : 0;
-  w.lo = a.window > 0 ? first + tok + 1 - a.window : 0;
-  // the wavefront's first and last row, and the tile's
-  const int32_t min_hi = first + row0 / a.group + 1;
-  const int32_t max_hi = n_rows > 0 ? first + (row0 + n_rows - 1) / a.group + 1 : 0;
-  const int32_t min_lo = a.window > 0 ? min_hi - a.window : 0;
-  const int32_t tile_min_hi = first + it.tile * MANY_ROWS / a.group + 1;
-  int32_t tile_end = (it.tile + 1) * MANY_ROWS;
-  if (tile_end > it.n_new * a.group) tile_end = it.n_new * a.group;
-  const int32_t tile_max_lo = a.window > 0 ? first + (tile_end - 1) / a.group + 1 - a.window : 0;
+    Rows<D> w;
+    const bool has_row = col < n_rows;
+    const int32_t row = row0 + col, tok = row / a.group, head = kvh * a.group + row % a.group;
+    const int32_t first = it.kv_len - it.n_new;  // the first new token's place
+    w.hi = has_row ? first + tok + 1 : 0;
+    w.lo = a.window > 0 ? first + tok + 1 - a.window : 0;
+    // the wavefront's first and last row, and the tile's
+    const int32_t min_hi = first + row0 / a.group + 1;
+    const int32_t max_hi = n_rows > 0 ? first + (row0 + n_rows - 1) / a.group + 1 : 0;
+    const int32_t min_lo = a.window > 0 ? min_hi - a.window : 0;
+    const int32_t tile_min_hi = first + it.tile * MANY_ROWS / a.group + 1;
+    int32_t tile_end = (it.tile + 1) * MANY_ROWS;
+    if (tile_end > it.n_new * a.group) tile_end = it.n_new * a.group;
+    const int32_t tile_max_lo = a.window > 0 ? first + (tile_end - 1) / a.group + 1 - a.window : 0;
 
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    w.q[s] = u32x4{0, 0, 0, 0};
-    if (has_row)
-      w.q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + s * 16 +
-                                                half * 8);
-  }
-#pragma unroll
-  for (int i = 0; i < DT; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) w.o[i][r] = 0.0f;
-  w.m = -INFINITY;
-  w.l = 0.0f;
-  const char *kbase = a.cache.k.base + kvh * a.cache.k.head;
-  const char *vbase = a.cache.v.base + kvh * a.cache.v.head;
-  const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
-  const float sc = a.scale_log2 * (KV8 && a.cache.k_scale ? a.cache.k_scale[kvh] : 1.0f);
-
-  const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
-  u32x4 kr[KV8 ? NL : 1], vr[KV8 ? NL : 1];  // 8-bit keys and values on their way to LDS
-  const int lrow = lane / LPR, lcol = lane % LPR;
-  bool bad_page = false;
-  // Where a place's keys and values are; a page outside the cache reads page 0.
-  const auto find = [&](int32_t key, uint64_t &kp, uint64_t &vp) {
-    const int32_t page = page_of(a.cache.ps, key);
-    int32_t id = table[page];
-    if (uint32_t(id) >= uint32_t(a.cache.n_pages)) {
-      id = 0;
-      bad_page = true;
+    for (int s = 0; s < STEPS; ++s) {
+      w.q[s] = u32x4{0, 0, 0, 0};
+      if (has_row)
+        w.q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + s * 16 +
+                                                  half * 8);
     }
-    const int32_t slot = key - page * a.cache.ps.size;
-    kp = reinterpret_cast<uint64_t>(kbase) + id * a.cache.k.page + slot * a.cache.k.token;
-    vp = reinterpret_cast<uint64_t>(vbase) + id * a.cache.v.page + slot * a.cache.v.token;
-  };
-  // WIDE: lane l knows where the 16 keys from known_from + 16 l on are, for 16 steps at a time
-  uint64_t kp_l = 0, vp_l = 0;
-  int32_t known_from = 0;
-  const auto find_steps = [&](int32_t kb) {
-    int32_t key = kb + 16 * lane;  // 16 keys outside [k0, k1) read a neighbour's places: in bounds, not seen
-    key = key < last_key ? key : last_key;
-    key = key > k0 ? key : k0;
-    find(key & ~15, kp_l, vp_l);
-    known_from = kb;
-  };
-  const uint32_t k_lane = uint32_t(lrow) * uint32_t(a.cache.k.token), v_lane = uint32_t(lrow) * uint32_t(a.cache.v.token);
-  // From memory: 16-bit rows straight to LDS, each lane fetching the piece that belongs where
-  // its 16 bytes land; 8-bit ones to registers, from which to_16 widens them.
-  const auto load_step = [&](int32_t kb, char *kl, char *vl) {
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int r = i * RPL + wave * RPW;  // the wavefront's first row
-      const int kc = KV8 ? lcol : lcol ^ ((r + lrow) & KSW), vc = KV8 ? lcol : lcol ^ (2 * ((r + lrow) & VSW));
-      uint64_t kp, vp;
-      uint32_t ko = kc * 16, vo = vc * 16;
-      if (WIDE) {
-        const int from = (kb - known_from + r) / 16;
-        kp = read_lane(kp_l, from);
-        vp = read_lane(vp_l, from);
-        ko += k_lane + uint32_t(r % 16) * uint32_t(a.cache.k.token);
-        vo += v_lane + uint32_t(r % 16) * uint32_t(a.cache.v.token);
-      } else {
-        int32_t key = kb + r + lrow;
-        key = key < last_key ? key : last_key;
-        key = key > k0 ? key : k0;
-        find(key, kp, vp);
-      }
-      const char *k = reinterpret_cast<const char *>(kp) + ko, *v = reinterpret_cast<const char *>(vp) + vo;
-      if (KV8) {
-        kr[i] = *reinterpret_cast<const u32x4 *>(k);
-        vr[i] = *reinterpret_cast<const u32x4 *>(v);
-      } else {
-        to_lds(k, kl + r * ROWB);
-        to_lds(v, vl + r * ROWB);
-      }
-    }
-  };
-  const auto to_16 = [&](char *kl, char *vl) {
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int r = i * RPL + wave * RPW + lrow;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 k = kr[i], v = vr[i];
-        const uint32_t x = h ? k.z : k.x, y = h ? k.w : k.y, z = h ? v.z : v.x, u = h ? v.w : v.y;
-        *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((2 * lcol + h) ^ (r & KSW)) * 16) =
-            u32x4{T::template from_e4m3<false>(x), T::template from_e4m3<true>(x), T::template from_e4m3<false>(y),
-                  T::template from_e4m3<true>(y)};
-        *reinterpret_cast<u32x4 *>(vl + r * ROWB + ((2 * lcol + h) ^ (2 * (r & VSW))) * 16) =
-            u32x4{T::template from_e4m3<false>(z), T::template from_e4m3<true>(z), T::template from_e4m3<false>(u),
-                  T::template from_e4m3<true>(u)};
-      }
-    }
-  };
-  // A step at the ends of what the rows see: values outside [k0, k1), which may be anything,
-  // become zeros; a value that is not finite marks the step.
-  const auto look_over = [&](int32_t kb, char *vl) {
-    constexpr int TPR = MT / KT, BYTES = ROWB / TPR;
-    const int r = threadIdx.x / TPR;
-    char *p = vl + r * ROWB + threadIdx.x % TPR * BYTES;
-    const bool in = kb + r >= k0 && kb + r < k1;
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < BYTES; i += 16) {
-      if (in)
-        odd |= any_not_finite<T>(*reinterpret_cast<const u32x4 *>(p + i));
-      else
-        *reinterpret_cast<u32x4 *>(p + i) = u32x4{0, 0, 0, 0};
-    }
-    if (odd) odd_step = kb;
-    __syncthreads();
-  };
-  const auto arrived = [] {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-  };
-  // One step: the next one's loads, this one's products.  ENDS: some row of the tile does not
-  // see all of its keys.
-  const auto turn = [&](auto ends, int32_t kb, char(&kl)[KT * ROWB], char(&vl)[KT * ROWB], char *k_next, char *v_next) {
-    constexpr bool ENDS = decltype(ends)::value;
-    const int32_t next = kb + KT;
-    if (next < k1) {
-      if (WIDE && next - known_from >= 64 * 16) find_steps(next);
-      load_step(next, k_next, v_next);
-    }
-    if (ENDS) look_over(kb, vl);
-    if (!ENDS || (kb < max_hi && kb + KT > min_lo)) step<T, D, ENDS>(w, kl, vl, kb, sc, ENDS && odd_step == kb, lane);
-    if (KV8 && next < k1) to_16(k_next, v_next);
-    arrived();
-  };
-
-  __syncthreads();  // odd_step is set before a step may mark it
-  if (kb0 < k1) {
-    // steps that every row sees whole; the others, and a lone one beside them, take the other form
-    const int32_t full0 = (max(k0, tile_max_lo) + KT - 1) / KT * KT, full1 = min(k1, tile_min_hi);
-    if (WIDE) find_steps(kb0);
-    load_step(kb0, k_even, v_even);
-    if (KV8) to_16(k_even, v_even);
-    arrived();
-    int32_t kb = kb0;
-    while (kb < k1) {
-      for (; kb >= full0 && kb + 2 * KT <= full1; kb += 2 * KT) {
-        turn(std::false_type{}, kb, k_even, v_even, k_odd, v_odd);
-        turn(std::false_type{}, kb + KT, k_odd, v_odd, k_even, v_even);
-      }
-      if (kb < k1) turn(std::true_type{}, kb, k_even, v_even, k_odd, v_odd);
-      kb += KT;
-      if (kb < k1) turn(std::true_type{}, kb, k_odd, v_odd, k_even, v_even);
-      kb += KT;
-    }
-  }
-  if (bad_page) set_status(a.status, SMETRIC_EINVAL);
-  {
-    const u32x2 both = swap32(__float_as_uint(w.l), __float_as_uint(w.l));
-    w.l = __uint_as_float(both.x) + __uint_as_float(both.y);
-  }
-  const float vs = KV8 && a.cache.v_scale ? a.cache.v_scale[kvh] : 1.0f;
-  if (it.part < 0) {
-    const float inv = w.l == 0.0f ? 0.0f : vs / w.l;
-    uint16_t *p = a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; g += 2) {
-        u32x4 x;
+      for (int r = 0; r < 16; ++r) w.o[i][r] = 0.0f;
+    w.m = -INFINITY;
+    w.l = 0.0f;
+    const char *kbase = a.cache.k.base + kvh * a.cache.k.head;
+    const char *vbase = a.cache.v.base + kvh * a.cache.v.head;
+    const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
+    const float sc = a.scale_log2 * (KV8 && a.cache.k_scale ? a.cache.k_scale[kvh] : 1.0f);
+
+    const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
+    u32x4 kr[KV8 ? NL : 1], vr[KV8 ? NL : 1];  // 8-bit keys and values on their way to LDS
+    const int lrow = lane / LPR, lcol = lane % LPR;
+    bool bad_page = false;
+    // Where a place's keys and values are; a page outside the cache reads page 0.
+    const auto find = [&](int32_t key, uint64_t &kp, uint64_t &vp) {
+      const int32_t page = page_of(a.cache.ps, key);
+      int32_t id = table[page];
+      if (uint32_t(id) >= uint32_t(a.cache.n_pages)) {
+        id = 0;
+        bad_page = true;
+      }
+      const int32_t slot = key - page * a.cache.ps.size;
+      kp = reinterpret_cast<uint64_t>(kbase) + id * a.cache.k.page + slot * a.cache.k.token;
+      vp = reinterpret_cast<uint64_t>(vbase) + id * a.cache.v.page + slot * a.cache.v.token;
+    };
+    // WIDE: lane l knows where the 16 keys from known_from + 16 l on are, for 16 steps at a time
+    uint64_t kp_l = 0, vp_l = 0;
+    int32_t known_from = 0;
+    const auto find_steps = [&](int32_t kb) {
+      int32_t key = kb + 16 * lane;  // 16 keys outside [k0, k1) read a neighbour's places: in bounds, not seen
+      key = key < last_key ? key : last_key;
+      key = key > k0 ? key : k0;
+      find(key & ~15, kp_l, vp_l);
+      known_from = kb;
+    };
+    const uint32_t k_lane = uint32_t(lrow) * uint32_t(a.cache.k.token), v_lane = uint32_t(lrow) * uint32_t(a.cache.v.token);
+    // From memory: 16-bit rows straight to LDS, each lane fetching the piece that belongs where
+    // its 16 bytes land; 8-bit ones to registers, from which to_16 widens them.
+    const auto load_step = [&](int32_t kb, char *kl, char *vl) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {  // halves trade 4 components: each then has 8 in a row
-          const u32x2 z = swap32(T::pack(w.o[i][4 * g + 2 * e] * inv, w.o[i][4 * g + 2 * e + 1] * inv),
-                                 T::pack(w.o[i][4 * g + 4 + 2 * e] * inv, w.o[i][4 * g + 4 + 2 * e + 1] * inv));
-          x[e] = z.x;
-          x[2 + e] = z.y;
+      for (int i = 0; i < NL; ++i) {
+        const int r = i * RPL + wave * RPW;  // the wavefront's first row
+        const int kc = KV8 ? lcol : lcol ^ ((r + lrow) & KSW), vc = KV8 ? lcol : lcol ^ (2 * ((r + lrow) & VSW));
+        uint64_t kp, vp;
+        uint32_t ko = kc * 16, vo = vc * 16;
+        if (WIDE) {
+          const int from = int(uint32_t(kb - known_from + r) / 16);
+          kp = read_lane(kp_l, from);
+          vp = read_lane(vp_l, from);
+          ko += k_lane + uint32_t(r % 16) * uint32_t(a.cache.k.token);
+          vo += v_lane + uint32_t(r % 16) * uint32_t(a.cache.v.token);
+        asm("" : "+v"(ko), "+v"(vo));  // stays a 32-bit offset to a scalar address
+        } else {
+          int32_t key = kb + r + lrow;
+          key = key < last_key ? key : last_key;
+          key = key > k0 ? key : k0;
+          find(key, kp, vp);
         }
-        if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
+        const char *k = reinterpret_cast<const char *>(kp) + ko, *v = reinterpret_cast<const char *>(vp) + vo;
+        if (KV8) {
+          kr[i] = *reinterpret_cast<const u32x4 *>(k);
+          vr[i] = *reinterpret_cast<const u32x4 *>(v);
+        } else {
+          to_lds(k, kl + r * ROWB);
+          to_lds(v, vl + r * ROWB);
+        }
       }
-    if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of<T>(w.m, w.l);
-  } else if (has_row) {
-    const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
+    };
+    const auto to_16 = [&](char *kl, char *vl) {
 #pragma unroll
-    for (int i = 0; i < DT; ++i)
+      for (int i = 0; i < NL; ++i) {
+        const int r = i * RPL + wave * RPW + lrow;
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + 32 * i + 8 * g + 4 * half) =
-            f32x4{w.o[i][4 * g] * vs, w.o[i][4 * g + 1] * vs, w.o[i][4 * g + 2] * vs, w.o[i][4 * g + 3] * vs};
-    if (half == 0) a.parts.ml[slot] = f32x2{w.m, w.l};
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 k = kr[i], v = vr[i];
+          const uint32_t x = h ? k.z : k.x, y = h ? k.w : k.y, z = h ? v.z : v.x, u = h ? v.w : v.y;
+          *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((2 * lcol + h) ^ (r & KSW)) * 16) =
+              u32x4{T::template from_e4m3<false>(x), T::template from_e4m3<true>(x), T::template from_e4m3<false>(y),
+                    T::template from_e4m3<true>(y)};
+          *reinterpret_cast<u32x4 *>(vl + r * ROWB + ((2 * lcol + h) ^ (2 * (r & VSW))) * 16) =
+              u32x4{T::template from_e4m3<false>(z), T::template from_e4m3<true>(z), T::template from_e4m3<false>(u),
+                    T::template from_e4m3<true>(u)};
+        }
+      }
+    };
+    // A step at the ends of what the rows see: values outside [k0, k1), which may be anything,
+    // become zeros; a value that is not finite marks the step.
+    const auto look_over = [&](int32_t kb, char *vl) {
+      constexpr int TPR = MT / KT, BYTES = ROWB / TPR;
+      const int r = threadIdx.x / TPR;
+      char *p = vl + r * ROWB + threadIdx.x % TPR * BYTES;
+      const bool in = kb + r >= k0 && kb + r < k1;
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < BYTES; i += 16) {
+        if (in)
+          odd |= any_not_finite<T>(*reinterpret_cast<const u32x4 *>(p + i));
+        else
+          *reinterpret_cast<u32x4 *>(p + i) = u32x4{0, 0, 0, 0};
+      }
+      if (odd) odd_step = kb;
+      __syncthreads();
+    };
+    const auto arrived = [] {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+    };
+    // One step: the next one's loads, this one's products.  ENDS: some row of the tile does not
+    // see all of its keys.
+    const auto turn = [&](auto ends, int32_t kb, char(&kl)[KT * ROWB], char(&vl)[KT * ROWB], char *k_next, char *v_next) {
+      constexpr bool ENDS = decltype(ends)::value;
+      const int32_t next = kb + KT;
+      if (next < k1) {
+        if (WIDE && next - known_from >= 64 * 16) find_steps(next);
+        load_step(next, k_next, v_next);
+      }
+      if (ENDS) look_over(kb, vl);
+      if (!ENDS || (kb < max_hi && kb + KT > min_lo)) step<T, D, ENDS>(w, kl, vl, kb, sc, ENDS && odd_step == kb, lane);
+      if (KV8 && next < k1) to_16(k_next, v_next);
+      arrived();
+    };
+
+    __syncthreads();  // odd_step is set before a step may mark it
+    if (kb0 < k1) {
+      // steps that every row sees whole; the others, and a lone one beside them, take the other form
+      const int32_t full0 = (max(k0, tile_max_lo) + KT - 1) / KT * KT, full1 = min(k1, tile_min_hi);
+      if (WIDE) find_steps(kb0);
+      load_step(kb0, k_even, v_even);
+      if (KV8) to_16(k_even, v_even);
+      arrived();
+      int32_t kb = kb0;
+      while (kb < k1) {
+        for (; kb >= full0 && kb + 2 * KT <= full1; kb += 2 * KT) {
+          turn(std::false_type{}, kb, k_even, v_even, k_odd, v_odd);
+          turn(std::false_type{}, kb + KT, k_odd, v_odd, k_even, v_even);
+        }
+        if (kb < k1) turn(std::true_type{}, kb, k_even, v_even, k_odd, v_odd);
+        kb += KT;
+        if (kb < k1) turn(std::true_type{}, kb, k_odd, v_odd, k_even, v_even);
+        kb += KT;
+      }
+    }
+    if (bad_page) set_status(a.status, SMETRIC_EINVAL);
+    {
+      const u32x2 both = swap32(__float_as_uint(w.l), __float_as_uint(w.l));
+      w.l = __uint_as_float(both.x) + __uint_as_float(both.y);
+    }
+    const float vs = KV8 && a.cache.v_scale ? a.cache.v_scale[kvh] : 1.0f;
+    if (it.part < 0) {
+      const float inv = w.l == 0.0f ? 0.0f : vs / w.l;
+      uint16_t *p = a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head;
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; g += 2) {
+          u32x4 x;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {  // halves trade 4 components: each then has 8 in a row
+            const u32x2 z = swap32(T::pack(w.o[i][4 * g + 2 * e] * inv, w.o[i][4 * g + 2 * e + 1] * inv),
+                                   T::pack(w.o[i][4 * g + 4 + 2 * e] * inv, w.o[i][4 * g + 4 + 2 * e + 1] * inv));
+            x[e] = z.x;
+            x[2 + e] = z.y;
+          }
+          if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
+        }
+      if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of<T>(w.m, w.l);
+    } else if (has_row) {
+      const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + 32 * i + 8 * g + 4 * half) =
+              f32x4{w.o[i][4 * g] * vs, w.o[i][4 * g + 1] * vs, w.o[i][4 * g + 2] * vs, w.o[i][4 * g + 3] * vs};
+      if (half == 0) a.parts.ml[slot] = f32x2{w.m, w.l};
+    }
   }
 }
 
 template <typename T, bool KV8, int D>
-int launch_d(const AttendArgs &a, int64_t max_items, hipStream_t stream) {
-  const dim3 grid(uint32_t(max_items * a.n_kv)), block(MT);
+int launch_d(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
+  const dim3 grid(uint32_t(max_groups * a.n_kv)), block(MT);
   if (a.cache.ps.size % 16 == 0)
     many_kernel<T, KV8, D, true><<<grid, block, 0, stream>>>(a);
   else
@@ -409,17 +404,17 @@ int launch_d(const AttendArgs &a, int64_t max_items, hipStream_t stream) {
   return hip_status(hipGetLastError());
 }
 template <typename T, bool KV8>
-int launch_k(const AttendArgs &a, int32_t d, int64_t max_items, hipStream_t stream) {
-  return d == 64 ? launch_d<T, KV8, 64>(a, max_items, stream)
-                 : d == 128 ? launch_d<T, KV8, 128>(a, max_items, stream) : launch_d<T, KV8, 256>(a, max_items, stream);
+int launch_k(const AttendArgs &a, int32_t d, int64_t max_groups, hipStream_t stream) {
+  return d == 64 ? launch_d<T, KV8, 64>(a, max_groups, stream)
+                 : d == 128 ? launch_d<T, KV8, 128>(a, max_groups, stream) : launch_d<T, KV8, 256>(a, max_groups, stream);
 }
 
 }  // namespace
 
-int launch_many(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_items, hipStream_t stream) {
+int launch_many(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
   if (dtype == SMETRIC_BF16)
-    return kv8 ? launch_k<Bf16, true>(a, head_dim, max_items, stream) : launch_k<Bf16, false>(a, head_dim, max_items, stream);
-  return kv8 ? launch_k<F16, true>(a, head_dim, max_items, stream) : launch_k<F16, false>(a, head_dim, max_items, stream);
+    return kv8 ? launch_k<Bf16, true>(a, head_dim, max_groups, stream) : launch_k<Bf16, false>(a, head_dim, max_groups, stream);
+  return kv8 ? launch_k<F16, true>(a, head_dim, max_groups, stream) : launch_k<F16, false>(a, head_dim, max_groups, stream);
 }
 
 }  // namespace smk

@@ -2,8 +2,8 @@
 // of the tiles whose keys were cut.
 //
 // The plan depends on the lengths alone, so one serves all layers of a step.  One workgroup
-// makes it: the total of the tiles' key steps gives the length of a piece, then every tile
-// writes its pieces at a place from a scan over the tiles.
+// makes it: it totals the tiles' costs (key steps, and what a tile costs besides), decides on
+// shares or whole tiles, and every tile writes its pieces at places from scans over the tiles.
 #include <math.h>
 
 #include "kv_attend.h"
@@ -11,144 +11,201 @@
 namespace smk {
 namespace {
 
-constexpr int PT = 1024;
+constexpr int PT = 512;
+constexpr int32_t STAGED = 2048;   // requests whose offsets and lengths are kept in LDS
+constexpr int32_t TILE_COST = 2;   // steps: a tile's queries, first pages and output
+constexpr int32_t CUT_COST = 12;   // steps: what a share's partial results cost, see whole_tiles
 
 struct PlanArgs {
   const int64_t *q_off;
   const int32_t *kv_len;
-  int32_t n_req, n_q, n_kv, group, rows, window, target, min_steps;
-  int64_t n_tokens, max_tiles, max_items, max_splits, max_parts;
+  int32_t n_req, n_q, n_kv, group, rows, rows_log2, window, target, min_steps, edge_steps;
+  int64_t n_tokens, max_tiles, max_items, max_groups, max_splits, max_parts;
   PlanHdr *hdr;
   PlanItem *items;
   PlanSplit *splits;
+  int32_t *first;
   int32_t *status;
 };
 
 struct Tile {
   int32_t req, tile, n_new, kv_len, tok0, k0, k1, steps;  // req < 0: the number belongs to no tile
 };
-__device__ Tile tile_at(const PlanArgs &a, int64_t g) {
+__device__ Tile tile_at(const PlanArgs &a, const int64_t *q_off, const int32_t *kv_len, int64_t g) {
   Tile t{-1, 0, 0, 0, 0, 0, 0, 0};
   int32_t lo = 0, hi = a.n_req - 1;  // the last request whose numbers begin at or before g
   while (lo < hi) {
     const int32_t mid = (lo + hi + 1) / 2;
-    if (a.q_off[mid] * a.group / a.rows + mid <= g)
+    if ((q_off[mid] * a.group >> a.rows_log2) + mid <= g)
       lo = mid;
     else
       hi = mid - 1;
   }
-  const int64_t q0 = a.q_off[lo];
-  const int64_t n = a.q_off[lo + 1] - q0, in = g - (q0 * a.group / a.rows + lo);
-  const int64_t tiles = (n * a.group + a.rows - 1) / a.rows;
+  const int64_t q0 = q_off[lo];
+  const int64_t n = q_off[lo + 1] - q0, in = g - ((q0 * a.group >> a.rows_log2) + lo);
+  const int64_t tiles = (n * a.group + a.rows - 1) >> a.rows_log2;
   if (in < 0 || in >= tiles) return t;
   t.req = lo;
   t.tile = int32_t(tiles - 1 - in);  // long ones first
   t.n_new = int32_t(n);
   t.tok0 = int32_t(q0);
-  t.kv_len = a.kv_len[lo];
-  const int32_t row0 = t.tile * a.rows;
-  int32_t last = row0 + a.rows;
-  if (last > t.n_new * a.group) last = t.n_new * a.group;
-  const int32_t first = t.kv_len - t.n_new + row0 / a.group;  // places of the tile's first and last token
-  t.k1 = t.kv_len - t.n_new + (last - 1) / a.group + 1;
+  t.kv_len = kv_len[lo];
+  const uint32_t row0 = uint32_t(t.tile) << a.rows_log2;
+  uint32_t last = row0 + a.rows;
+  if (last > uint32_t(t.n_new) * a.group) last = uint32_t(t.n_new) * a.group;
+  const int32_t first = t.kv_len - t.n_new + int32_t(row0 / uint32_t(a.group));  // places of the tile's first and last token
+  t.k1 = t.kv_len - t.n_new + int32_t((last - 1) / uint32_t(a.group)) + 1;
   t.k0 = a.window > 0 && first - a.window + 1 > 0 ? first - a.window + 1 : 0;
   if (t.k1 <= t.k0) t.k0 = t.k1 = 0;
   t.steps = (t.k1 + KEY_STEP - 1) / KEY_STEP - t.k0 / KEY_STEP;
   return t;
 }
 
-// Sums of v over the workgroup's earlier threads, and of all, for two counts at once.
-__device__ void scan2(int32_t &x, int32_t &y, int32_t &tx, int32_t &ty, int32_t (*sh)[PT / 64]) {
+// floor(x / d) for 0 <= x < 2^52: a quotient in 64-bit floats is at most one off.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t d) {
+  int64_t q = int64_t(double(x) / double(d));
+  q -= q * d > x;
+  q += (q + 1) * d <= x;
+  return q;
+}
+
+// Sum of x over the workgroup's earlier threads; total: over all.
+template <typename N>
+__device__ N scan(N x, N &total, N *sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int32_t a = x, b = y;
+  N a = x;
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) {
-    const int32_t ua = __shfl_up(a, m, 64), ub = __shfl_up(b, m, 64);
-    if (lane >= m) {
-      a += ua;
-      b += ub;
-    }
+    const N u = __shfl_up(a, m, 64);
+    if (lane >= m) a += u;
   }
-  if (lane == 63) {
-    sh[0][wave] = a;
-    sh[1][wave] = b;
-  }
+  if (lane == 63) sh[wave] = a;
   __syncthreads();
-  int32_t pa = 0, pb = 0;
-  tx = ty = 0;
+  N before = 0;
+  total = 0;
   for (int w = 0; w < PT / 64; ++w) {
-    if (w == wave) {
-      pa = tx;
-      pb = ty;
-    }
-    tx += sh[0][w];
-    ty += sh[1][w];
+    const N v = sh[w];
+    before += w < wave ? v : 0;
+    total += v;
   }
-  x = pa + a - x;
-  y = pb + b - y;
   __syncthreads();
+  return before + a - x;
+}
+
+// Whether each tile gets a workgroup of its own.  Estimates, in steps: with n workgroups at
+// once, whole tiles take ceil(tiles / n) rounds of the mean, at least the longest; or, as
+// early ends are filled, the even share and half the longest.  Shares take the even share
+// and what their cuts cost: partial sums written, read and joined, and a tile's start.
+__device__ bool whole_tiles(int64_t cost, int64_t tiles, int32_t longest, int32_t n) {
+  const int64_t share = quotient(cost + n - 1, n), rounds = quotient(tiles + n - 1, n);
+  int64_t whole = tiles > 0 ? rounds * quotient(cost + tiles - 1, tiles) : 0;
+  if (rounds > 1 && whole > share + longest / 2) whole = share + longest / 2;
+  if (whole < longest) whole = longest;
+  return whole <= share + CUT_COST;
 }
 
 __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
-  __shared__ int32_t sh[2][PT / 64];
-  __shared__ unsigned long long total;
-  __shared__ int bad;
-  if (threadIdx.x == 0) {
-    total = 0;
-    bad = 0;
-  }
+  static_assert(FEW_ROWS == 1 << 4 && MANY_ROWS == 1 << 7, "rows_log2");
+  __shared__ int64_t sh64[PT / 64];
+  __shared__ int32_t sh32[PT / 64];
+  __shared__ int64_t off_l[STAGED + 1];
+  __shared__ int32_t len_l[STAGED];
+  __shared__ int bad, longest;
+  if (threadIdx.x == 0) bad = longest = 0;
   __syncthreads();
   bool wrong = false;
+  const bool staged = a.n_req <= STAGED;
   for (int32_t r = threadIdx.x; r < a.n_req; r += PT) {
     const int64_t q0 = a.q_off[r], q1 = a.q_off[r + 1];
     const int32_t len = a.kv_len[r];
     wrong |= q0 < 0 || q1 < q0 || q1 > a.n_tokens || (r == 0 && q0 != 0) || (r == a.n_req - 1 && q1 != a.n_tokens) ||
              len < 0 || len > MAX_PLACES;
+    if (staged) {
+      off_l[r + 1] = q1;
+      len_l[r] = len;
+      if (r == 0) off_l[0] = q0;
+    }
   }
   if (wrong) bad = 1;
   __syncthreads();
-  int32_t n_items = 0, n_splits = 0, n_parts = 0;
+  const int64_t *q_off = staged ? off_l : a.q_off;
+  const int32_t *kv_len = staged ? len_l : a.kv_len;
+  int64_t n_items = 0, n_splits = 0, n_parts = 0, n_groups = 0;
   if (!bad) {
-    unsigned long long mine = 0;
-    for (int64_t g = threadIdx.x; g < a.max_tiles; g += PT) mine += tile_at(a, g).steps;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) mine += __shfl_xor(mine, m, 64);
-    if ((threadIdx.x & 63) == 0) atomicAdd(&total, mine);
-    __syncthreads();
-    const int64_t share = int64_t((total + a.target - 1) / a.target);
-    const int32_t piece = share < a.min_steps ? a.min_steps : int32_t(share);
+    int64_t mine = 0;
+    int32_t top = 0, count = 0;
+    Tile t{};
+    for (int64_t g = threadIdx.x; g < a.max_tiles; g += PT) {
+      t = tile_at(a, q_off, kv_len, g);
+      if (t.req < 0) continue;
+      const int32_t c = t.steps + TILE_COST;
+      mine += c;
+      top = c > top ? c : top;
+      ++count;
+    }
+    atomicMax(&longest, top);
+    int64_t cost, tiles;
+    scan<int64_t>(mine, cost, sh64);
+    scan<int64_t>(count, tiles, sh64);
+    const int32_t least = a.min_steps + TILE_COST;
+    int64_t groups = quotient(cost + least - 1, least);
+    if (groups > a.target) groups = a.target;
+    if (groups < 1) groups = 1;
+    const int64_t share = cost > 0 ? quotient(cost + groups - 1, groups) : 1;
+    const bool whole = whole_tiles(cost, tiles, longest, a.target);
+    n_groups = whole ? tiles : quotient(cost + share - 1, share);
+    const int32_t edge = a.edge_steps + TILE_COST;
+    int64_t at0 = 0;
     for (int64_t g0 = 0; g0 < a.max_tiles; g0 += PT) {
       const int64_t g = g0 + threadIdx.x;
-      Tile t{-1, 0, 0, 0, 0, 0, 0, 0};
-      if (g < a.max_tiles) t = tile_at(a, g);
-      const int32_t pieces = t.req < 0 ? 0 : t.steps <= piece ? 1 : (t.steps + piece - 1) / piece;
-      int32_t at = pieces, cut = pieces > 1 ? pieces : 0, cut_at = cut, all, all_cut;
-      scan2(at, cut_at, all, all_cut, sh);
-      int32_t split = pieces > 1, none = 0, split_at, t0, t1;
-      split_at = split;
-      scan2(split_at, none, t0, t1, sh);
-      const int32_t base = n_items + at, part0 = n_parts + cut_at;
-      // even pieces: the last is not the shortest by much
-      for (int32_t i = 0; i < pieces && base + i < a.max_items; ++i) {
-        const int64_t s0 = int64_t(t.steps) * i / pieces, s1 = int64_t(t.steps) * (i + 1) / pieces;
-        const int32_t k = t.k0 / KEY_STEP * KEY_STEP;
-        a.items[base + i] =
-            PlanItem{t.req,  t.tok0, t.n_new, t.kv_len, t.tile, i == 0 ? t.k0 : int32_t(k + s0 * KEY_STEP),
-                     i == pieces - 1 ? t.k1 : int32_t(k + s1 * KEY_STEP), cut ? part0 + i : -1};
+      if (a.max_tiles > PT || g >= a.max_tiles) t.req = -1;
+      if (a.max_tiles > PT && g < a.max_tiles) t = tile_at(a, q_off, kv_len, g);
+      const int64_t c = t.req < 0 ? 0 : t.steps + TILE_COST;
+      int64_t all;
+      const int64_t at = at0 + scan<int64_t>(c, all, sh64);
+      at0 += all;
+      // shares' ends at multiples of `share`: w_lo .. w_hi cut this tile
+      int64_t w_lo = 0, w_hi = -1;
+      if (t.req >= 0 && !whole) {
+        w_lo = quotient(at + edge + share - 1, share);
+        w_hi = at + c < edge ? -1 : quotient(at + c - edge, share);
+        if (w_hi >= n_groups) w_hi = n_groups - 1;
       }
-      if (split && n_splits + split_at < a.max_splits)
-        a.splits[n_splits + split_at] = PlanSplit{t.tok0, t.n_new, t.tile, part0, pieces, {0, 0, 0}};
-      n_items += all;
-      n_parts += all_cut;
-      n_splits += t0;
+      const int32_t cuts = w_hi >= w_lo ? int32_t(w_hi - w_lo + 1) : 0, pieces = t.req < 0 ? 0 : cuts + 1;
+      int32_t all_p, all_c, all_s;
+      const int64_t base = n_items + scan<int32_t>(pieces, all_p, sh32);
+      const int64_t part0 = n_parts + scan<int32_t>(cuts ? pieces : 0, all_c, sh32);
+      const int64_t split_at = n_splits + scan<int32_t>(cuts > 0, all_s, sh32);
+      const int32_t k = t.k0 / KEY_STEP;
+      for (int32_t i = 0; i < pieces && base + i < a.max_items; ++i) {
+        const int32_t c0 = i ? int32_t((w_lo + i - 1) * share - at) - TILE_COST : 0;
+        const int32_t c1 = i < cuts ? int32_t((w_lo + i) * share - at) - TILE_COST : 0;
+        a.items[base + i] = PlanItem{t.req, t.tok0, t.n_new, t.kv_len, t.tile, i == 0 ? t.k0 : (k + c0) * KEY_STEP,
+                                     i == cuts ? t.k1 : (k + c1) * KEY_STEP, cuts ? int32_t(part0 + i) : -1};
+      }
+      if (cuts && split_at < a.max_splits)
+        a.splits[split_at] = PlanSplit{t.tok0, t.n_new, t.tile, int32_t(part0), pieces, {0, 0, 0}};
+      if (t.req >= 0 && whole) {
+        if (base < a.max_groups) a.first[base] = int32_t(base);
+      } else if (t.req >= 0) {  // the workgroups whose shares begin in this tile
+        for (int64_t w = quotient(at + share - 1, share); w * share < at + c && w < n_groups && w < a.max_groups; ++w)
+          a.first[w] = int32_t(base + (w < w_lo ? 0 : w > w_hi ? pieces : w - w_lo + 1));
+      }
+      n_items += all_p;
+      n_parts += all_c;
+      n_splits += all_s;
     }
   }
   if (threadIdx.x == 0) {
     PlanHdr h{};
     h.err = bad ? SMETRIC_EINVAL : SMETRIC_OK;
-    if (n_items > a.max_items || n_splits > a.max_splits || n_parts > a.max_parts) h.err = SMETRIC_EINTERNAL;
-    h.n_items = n_items;
-    h.n_splits = n_splits;
+    if (n_items > a.max_items || n_splits > a.max_splits || n_parts > a.max_parts || n_groups > a.max_groups)
+      h.err = SMETRIC_EINTERNAL;
+    else
+      a.first[n_groups] = int32_t(n_items);
+    h.n_items = int32_t(n_items);
+    h.n_splits = int32_t(n_splits);
+    h.n_groups = int32_t(n_groups);
     h.n_req = a.n_req;
     h.n_q = a.n_q;
     h.n_kv = a.n_kv;
@@ -161,70 +218,91 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
 }
 
 // Joins the parts of a cut tile: out = sum_p 2^(m_p - m) acc_p / sum_p 2^(m_p - m) l_p, in the
-// order of the parts.  A workgroup takes one row of one key-value head at a time: D / 4
-// threads a part, several parts side by side.
-constexpr int32_t JOIN_GRID = 1024;
+// order of the parts.  D / 4 threads hold a row.  Tiles of many rows: the workgroup takes as
+// many rows at once (each of a few parts).  Tiles of few rows, which may have hundreds of
+// parts: it takes one row's parts side by side.
+constexpr int32_t JOIN_GRID = 2048;
 template <typename T, int D>
+__device__ __forceinline__ void write_row(const AttendArgs &a, const PlanSplit &s, int32_t in_req, int32_t kvh, int sub,
+                                          f32x4 acc, float m, float l) {
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int64_t t = int64_t(s.tok0) + in_req / a.group;
+  const int32_t head = kvh * a.group + in_req % a.group;
+  *reinterpret_cast<u32x2 *>(a.out.data + t * a.out.token + head * a.out.head + sub * 4) =
+      u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
+  if (a.lse && sub == 0) a.lse[t * a.n_q + head] = lse_of<T>(m, l);
+}
+template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
-  constexpr int TPP = D / 4, SIDE = 256 / TPP;
+  constexpr int TPP = D / 4, SIDE = 256 / TPP, BLOCKS = FEW ? FEW_ROWS : MANY_ROWS / SIDE;
   __shared__ f32x4 sh[256];
   __shared__ float shl[SIDE];
-  if (!plan_fits(a)) return;
-  const int64_t units = int64_t(a.hdr->n_splits) * a.n_kv * a.rows;
+  const PlanHdr h = *a.hdr;
+  if (!plan_fits(a, h)) return;
+  const int64_t units = int64_t(h.n_splits) * a.n_kv * BLOCKS;
   const int32_t sub = threadIdx.x % TPP, side = threadIdx.x / TPP;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int32_t kvh = int32_t(u % a.n_kv), row = int32_t(u / a.n_kv % a.rows);
-    const PlanSplit s = a.splits[u / a.n_kv / a.rows];
+    const int32_t kvh = int32_t(u % a.n_kv), block = int32_t(u / a.n_kv % BLOCKS);
+    const PlanSplit s = a.splits[u / a.n_kv / BLOCKS];
+    const int32_t row = FEW ? block : block * SIDE + side;
     const int32_t in_req = s.tile * a.rows + row;
-    if (in_req >= s.n_new * a.group) continue;
-    const int64_t step = int64_t(a.n_kv) * a.rows, at0 = (int64_t(s.part0) * a.n_kv + kvh) * a.rows + row;
+    const int64_t step = int64_t(a.n_kv) * a.rows, at = (int64_t(s.part0) * a.n_kv + kvh) * a.rows + row;
+    if (in_req >= s.n_new * a.group) continue;  // (FEW: the whole workgroup)
+    const f32x2 *ml = a.parts.ml + at;
+    const float *parts = a.parts.acc + at * D + sub * 4;
     float m = -INFINITY;
-    for (int32_t p = threadIdx.x & 63; p < s.n_parts; p += 64) m = fmaxf(m, a.parts.ml[at0 + p * step].x);
+    if (FEW) {
+      for (int32_t p = threadIdx.x & 63; p < s.n_parts; p += 64) m = fmaxf(m, ml[p * step].x);
 #pragma unroll
-    for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i, 64));
+      for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i, 64));
+    } else {
+      for (int32_t p = 0; p < s.n_parts; ++p) m = fmaxf(m, ml[p * step].x);
+    }
     const float ms = m == -INFINITY ? 0.0f : m;
     f32x4 acc{0, 0, 0, 0};
     float l = 0.0f;
 #pragma unroll 4
-    for (int32_t p = side; p < s.n_parts; p += SIDE) {
-      const f32x2 ml = a.parts.ml[at0 + p * step];
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(a.parts.acc + (at0 + p * step) * D + sub * 4);
-      const float w = exp2f(ml.x - ms);
-      l = fmaf(w, ml.y, l);
+    for (int32_t p = FEW ? side : 0; p < s.n_parts; p += FEW ? SIDE : 1) {
+      const f32x2 x = ml[p * step];
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(parts + p * step * D);
+      const float w = exp2f(x.x - ms);
+      l = fmaf(w, x.y, l);
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] = fmaf(w, v[i], acc[i]);
     }
-    sh[threadIdx.x] = acc;
-    if (sub == 0) shl[side] = l;
-    __syncthreads();
-    if (side == 0) {
+    if (FEW) {
+      sh[threadIdx.x] = acc;
+      if (sub == 0) shl[side] = l;
+      __syncthreads();
+      if (side == 0) {
 #pragma unroll
-      for (int i = 1; i < SIDE; ++i) {
-        acc += sh[i * TPP + sub];
-        l += shl[i];
+        for (int i = 1; i < SIDE; ++i) {
+          acc += sh[i * TPP + sub];
+          l += shl[i];
+        }
       }
-      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-      const int64_t t = int64_t(s.tok0) + in_req / a.group;
-      const int32_t head = kvh * a.group + in_req % a.group;
-      *reinterpret_cast<u32x2 *>(a.out.data + t * a.out.token + head * a.out.head + sub * 4) =
-          u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
-      if (a.lse && sub == 0) a.lse[t * a.n_q + head] = lse_of<T>(m, l);
     }
-    __syncthreads();
+    if (!FEW || side == 0) write_row<T, D>(a, s, in_req, kvh, sub, acc, m, l);
+    if (FEW) __syncthreads();
   }
 }
 
+template <typename T, int D>
+int launch_join_d(const AttendArgs &a, int64_t max_splits, hipStream_t stream) {
+  constexpr int SIDE = 256 / (D / 4);
+  const bool few = a.rows == FEW_ROWS;
+  const int64_t units = max_splits * a.n_kv * (few ? FEW_ROWS : MANY_ROWS / SIDE);
+  const dim3 grid(uint32_t(units < JOIN_GRID ? units : JOIN_GRID));
+  if (few)
+    join_kernel<T, D, true><<<grid, 256, 0, stream>>>(a);
+  else
+    join_kernel<T, D, false><<<grid, 256, 0, stream>>>(a);
+  return hip_status(hipGetLastError());
+}
 template <typename T>
 int launch_join(const AttendArgs &a, int32_t head_dim, int64_t max_splits, hipStream_t stream) {
-  const int64_t units = max_splits * a.n_kv * a.rows;
-  const dim3 grid(uint32_t(units < JOIN_GRID ? units : JOIN_GRID));
-  if (head_dim == 64)
-    join_kernel<T, 64><<<grid, 256, 0, stream>>>(a);
-  else if (head_dim == 128)
-    join_kernel<T, 128><<<grid, 256, 0, stream>>>(a);
-  else
-    join_kernel<T, 256><<<grid, 256, 0, stream>>>(a);
-  return hip_status(hipGetLastError());
+  return head_dim == 64 ? launch_join_d<T, 64>(a, max_splits, stream)
+                        : head_dim == 128 ? launch_join_d<T, 128>(a, max_splits, stream) : launch_join_d<T, 256>(a, max_splits, stream);
 }
 
 bool shape_ok(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t max_new) {
@@ -256,10 +334,11 @@ extern "C" int smetric_attend_plan(const int64_t *q_off, const int32_t *kv_len, 
   const PlanShape s = plan_shape(n_req, n_tokens, n_q_heads, n_kv_heads, head_dim, max_new);
   if (plan_bytes < s.plan_bytes) return SMETRIC_EWORKSPACE;
   char *p = static_cast<char *>(plan);
-  PlanArgs a{q_off, kv_len, n_req, n_q_heads, n_kv_heads, n_q_heads / n_kv_heads, s.rows, window, s.target,
-             (s.rows == FEW_ROWS ? FEW_MIN_KEYS : MANY_MIN_KEYS) / KEY_STEP, n_tokens, n_req ? s.max_tiles : 0,
-             s.max_items, s.max_splits, s.max_parts, reinterpret_cast<PlanHdr *>(p),
-             reinterpret_cast<PlanItem *>(p + s.off_items), reinterpret_cast<PlanSplit *>(p + s.off_splits), status};
+  PlanArgs a{q_off, kv_len, n_req, n_q_heads, n_kv_heads, n_q_heads / n_kv_heads, s.rows, s.rows == FEW_ROWS ? 4 : 7, window, s.target,
+             s.rows == FEW_ROWS ? FEW_MIN_STEPS : MANY_MIN_STEPS, s.rows == FEW_ROWS ? FEW_EDGE_STEPS : MANY_EDGE_STEPS,
+             n_tokens, n_req ? s.max_tiles : 0, s.max_items, s.max_groups, s.max_splits, s.max_parts,
+             reinterpret_cast<PlanHdr *>(p), reinterpret_cast<PlanItem *>(p + s.off_items),
+             reinterpret_cast<PlanSplit *>(p + s.off_splits), reinterpret_cast<int32_t *>(p + s.off_first), status};
   plan_kernel<<<1, PT, 0, stream>>>(a);
   return hip_status(hipGetLastError());
 }
@@ -278,12 +357,13 @@ extern "C" int smetric_attend(int32_t dtype, const smetric_kv_cache *cache, cons
   const PlanShape s =
       plan_shape(batch->n_req, batch->n_tokens, n_q_heads, cache->n_kv_heads, cache->head_dim, max_new);
   if (plan_bytes < s.plan_bytes || ws_bytes < s.ws_bytes || !workspace) return SMETRIC_EWORKSPACE;
-  if (s.max_items * cache->n_kv_heads > 0x7FFFFFFF) return SMETRIC_EINVAL;
+  if (s.max_groups * cache->n_kv_heads > 0x7FFFFFFF) return SMETRIC_EINVAL;
   const char *p = static_cast<const char *>(plan);
   AttendArgs a{};
   a.hdr = reinterpret_cast<const PlanHdr *>(p);
   a.items = reinterpret_cast<const PlanItem *>(p + s.off_items);
   a.splits = reinterpret_cast<const PlanSplit *>(p + s.off_splits);
+  a.first = reinterpret_cast<const int32_t *>(p + s.off_first);
   a.cache = cache_view(cache, batch);
   a.q = heads_view(q);
   a.out = heads_view(out);
@@ -301,8 +381,8 @@ extern "C" int smetric_attend(int32_t dtype, const smetric_kv_cache *cache, cons
   a.scale_log2 = scale * 1.4426950408889634f;
   a.status = status;
   const bool kv8 = cache->dtype == SMETRIC_E4M3;
-  int rc = s.rows == FEW_ROWS ? launch_few(a, dtype, kv8, cache->head_dim, s.max_items, stream)
-                              : launch_many(a, dtype, kv8, cache->head_dim, s.max_items, stream);
+  int rc = s.rows == FEW_ROWS ? launch_few(a, dtype, kv8, cache->head_dim, s.max_groups, stream)
+                              : launch_many(a, dtype, kv8, cache->head_dim, s.max_groups, stream);
   if (rc != SMETRIC_OK) return rc;
   return dtype == SMETRIC_BF16 ? launch_join<Bf16>(a, cache->head_dim, s.max_splits, stream)
                                : launch_join<F16>(a, cache->head_dim, s.max_splits, stream);
