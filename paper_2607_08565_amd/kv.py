@@ -12,7 +12,7 @@ Tensors go in by data pointer on torch's current stream; there is no CPU fallbac
 from __future__ import annotations
 
 import ctypes as C
-import math
+import struct
 
 import torch
 
@@ -21,8 +21,10 @@ from .smetric import EINVAL, SmetricError, _check, _dev, _lib, _stream
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
 
 
-class _Heads(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+# A single token's calls are bound by this file.  smetric_heads and smetric_batch go as packed
+# bytes: a ctypes structure takes 0.6 us to make, these 0.05 (five of them in an append).
+_pack_heads = struct.Struct("Pqq").pack      # data, token_stride, head_stride
+_pack_batch = struct.Struct("PqiiPPq").pack  # table, table_stride, max_pages, n_req, q_off, kv_len, n_tokens
 
 
 class _Cache(C.Structure):
@@ -31,46 +33,38 @@ class _Cache(C.Structure):
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
-class _Batch(C.Structure):
-    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("n_req", C.c_int32),
-                ("q_off", C.c_void_p), ("kv_len", C.c_void_p), ("n_tokens", C.c_int64)]
-
-
 class _Rotary(C.Structure):
     _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("table", C.c_void_p), ("n_pos", C.c_int64),
                 ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float)]
 
 
-def _heads(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str) -> _Heads:
+def _heads(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str) -> bytes:
     """An activation [tokens, heads, head_dim]; components contiguous, other strides any."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda:
         raise TypeError(f"{name}: expected a {dtype} CUDA tensor")
-    if tuple(t.shape) != shape or t.stride(2) != 1:
-        raise ValueError(f"{name}: expected shape {shape} with contiguous components, got {tuple(t.shape)}, "
-                         f"strides {t.stride()}")
-    return _Heads(t.data_ptr(), t.stride(0), t.stride(1))
+    st = t.stride()
+    if t.shape != shape or st[2] != 1:
+        raise ValueError(f"{name}: expected shape {tuple(shape)} with contiguous components, got {tuple(t.shape)}, "
+                         f"strides {st}")
+    return _pack_heads(t.data_ptr(), st[0], st[1])
 
 
 def _opt(t: torch.Tensor | None, dtype: torch.dtype, name: str):
     return None if t is None else _dev(t, dtype, name)
 
 
-def _page_table(t: torch.Tensor, n_req: int) -> torch.Tensor:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2:
+def _batch(t: torch.Tensor, q_off: torch.Tensor, kv_len: torch.Tensor, n_tokens: int) -> bytes:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or not t.is_cuda or t.dim() != 2:
         raise TypeError("page_table: expected an int32 CUDA matrix")
-    if t.shape[0] != n_req or (t.shape[1] > 1 and t.stride(1) != 1):
+    rows, width = t.shape
+    stride = t.stride()
+    n_req = kv_len.shape[0]
+    if rows != n_req or (width > 1 and stride[1] != 1):
         raise ValueError(f"page_table: expected {n_req} rows of contiguous entries, got {tuple(t.shape)}")
-    return t
-
-
-def _batch(page_table: torch.Tensor, q_off: torch.Tensor, kv_len: torch.Tensor, n_tokens: int) -> _Batch:
-    n_req = kv_len.numel()
-    if q_off.numel() != n_req + 1:
+    if q_off.shape[0] != n_req + 1:
         raise ValueError("q_off: expected one entry more than kv_len")
-    t = _page_table(page_table, n_req)
-    stride = max(t.stride(0), t.shape[1]) if n_req < 2 else t.stride(0)
-    return _Batch(t.data_ptr(), stride, t.shape[1], n_req, _dev(q_off, torch.int64, "q_off"),
-                  _dev(kv_len, torch.int32, "kv_len"), n_tokens)
+    return _pack_batch(t.data_ptr(), max(stride[0], width) if n_req < 2 else stride[0], width, n_req,
+                       _dev(q_off, torch.int64, "q_off"), _dev(kv_len, torch.int32, "kv_len"), n_tokens)
 
 
 class PagedCache:
@@ -122,11 +116,15 @@ class Rotary:
         self.c = _Rotary(w[0], w[1], _opt(table, torch.float32, "table") if rot_dim else None,
                          table.shape[0] if rot_dim else 0, rot_dim, int(interleaved), eps)
         self.ref = C.addressof(self.c)
+        self.fits = None  # the type and head_dim that the weights were found to fit
 
     def check(self, dtype: torch.dtype, head_dim: int):
+        if self.fits == (dtype, head_dim):
+            return
         for w, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
             if w is not None and (w.dtype != dtype or w.numel() != head_dim):
                 raise ValueError(f"{name}: expected {head_dim} values of {dtype}")
+        self.fits = (dtype, head_dim)
 
 
 def _type_of(t: torch.Tensor, name: str) -> int:
@@ -143,18 +141,18 @@ def qk_rotate(q: torch.Tensor, k: torch.Tensor, rotary: Rotary, positions: torch
               q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, status: torch.Tensor | None = None):
     """smetric_qk_rotate: queries and keys [tokens, heads, head_dim] normed and rotated to
     their positions (int32).  Outputs may be the inputs.  Returns (q_out, k_out)."""
-    dtype = _type_of(q, "q")
-    T, _, D = q.shape
-    rotary.check(q.dtype, D)
+    code, dtype, shape = _type_of(q, "q"), q.dtype, q.shape
+    T, Hq, D = shape
+    rotary.check(dtype, D)
     q_out = _new(q) if q_out is None else q_out
     k_out = _new(k) if k_out is None else k_out
-    if positions is not None and positions.numel() != T:
+    if positions is not None and positions.shape[0] != T:
         raise ValueError("positions: expected one per token")
-    a, b = _heads(q, q.dtype, tuple(q.shape), "q"), _heads(q_out, q.dtype, tuple(q.shape), "q_out")
-    c, d = _heads(k, q.dtype, (T, k.shape[1], D), "k"), _heads(k_out, q.dtype, (T, k.shape[1], D), "k_out")
+    k_shape = (T, k.shape[1], D)
     _check("smetric_qk_rotate", _lib.smetric_qk_rotate(
-        dtype, D, T, rotary.ref, _opt(positions, torch.int32, "positions"), q.shape[1], C.addressof(a), C.addressof(b),
-        k.shape[1], C.addressof(c), C.addressof(d), _opt(status, torch.int32, "status"), _stream()))
+        code, D, T, rotary.ref, _opt(positions, torch.int32, "positions"), Hq, _heads(q, dtype, shape, "q"),
+        _heads(q_out, dtype, shape, "q_out"), k_shape[1], _heads(k, dtype, k_shape, "k"),
+        _heads(k_out, dtype, k_shape, "k_out"), _opt(status, torch.int32, "status"), _stream()))
     return q_out, k_out
 
 
@@ -164,23 +162,24 @@ def append(cache: PagedCache, page_table: torch.Tensor, q_off: torch.Tensor, kv_
     """smetric_kv_append: the new tokens' keys (normed and rotated) and values into the pages;
     kv_len counts the new tokens already.  With q its queries normed and rotated are
     returned (q_out, may be q)."""
-    dtype = _type_of(k, "k")
-    T, H, D = k.shape[0], cache.n_kv_heads, cache.head_dim
+    code, dtype = _type_of(k, "k"), k.dtype
+    T, D = k.shape[0], cache.head_dim
+    shape = (T, cache.n_kv_heads, D)
+    ref = None
     if rotary is not None:
-        rotary.check(k.dtype, D)
-    batch = _batch(page_table, q_off, kv_len, T)
-    a, b = _heads(k, k.dtype, (T, H, D), "k"), _heads(v, k.dtype, (T, H, D), "v")
-    c = d = None
+        rotary.check(dtype, D)
+        ref = rotary.ref
+    if positions is not None and positions.shape[0] != T:
+        raise ValueError("positions: expected one per token")
+    Hq, q_in, q_to = 0, None, None
     if q is not None:
         q_out = _new(q) if q_out is None else q_out
-        shape = (T, q.shape[1], D)
-        c, d = _heads(q, k.dtype, shape, "q"), _heads(q_out, k.dtype, shape, "q_out")
-    if positions is not None and positions.numel() != T:
-        raise ValueError("positions: expected one per token")
+        Hq = q.shape[1]
+        q_shape = (T, Hq, D)
+        q_in, q_to = _heads(q, dtype, q_shape, "q"), _heads(q_out, dtype, q_shape, "q_out")
     _check("smetric_kv_append", _lib.smetric_kv_append(
-        dtype, cache.ref, C.addressof(batch), None if rotary is None else rotary.ref,
-        _opt(positions, torch.int32, "positions"), 0 if q is None else q.shape[1], c and C.addressof(c),
-        d and C.addressof(d), C.addressof(a), C.addressof(b), _opt(status, torch.int32, "status"), _stream()))
+        code, cache.ref, _batch(page_table, q_off, kv_len, T), ref, _opt(positions, torch.int32, "positions"), Hq, q_in,
+        q_to, _heads(k, dtype, shape, "k"), _heads(v, dtype, shape, "v"), _opt(status, torch.int32, "status"), _stream()))
     return q_out if q is not None else None
 
 
@@ -200,6 +199,7 @@ class Plan:
         if workspace is not None and workspace.numel() < self.ws_bytes:
             raise SmetricError("smetric_attend_plan_bytes", EINVAL)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device) if workspace is None else workspace
+        self.plan_ptr, self.ws_ptr = self.mem.data_ptr(), self.workspace.data_ptr()
         self.q_off = self.kv_len = None
 
     def make(self, q_off: torch.Tensor, kv_len: torch.Tensor, status: torch.Tensor | None = None) -> "Plan":
@@ -210,7 +210,7 @@ class Plan:
         self.q_off, self.kv_len = q_off, kv_len
         _check("smetric_attend_plan", _lib.smetric_attend_plan(
             _dev(q_off, torch.int64, "q_off"), _dev(kv_len, torch.int32, "kv_len"), *self.args, self.window,
-            self.mem.data_ptr(), self.plan_bytes, _opt(status, torch.int32, "status"), _stream()))
+            self.plan_ptr, self.plan_bytes, _opt(status, torch.int32, "status"), _stream()))
         return self
 
 
@@ -219,19 +219,19 @@ def attend(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, plan: P
     """smetric_attend: the new tokens' attention over the pages, as `plan` (made for the batch)
     splits it.  scale: 1 / sqrt(head_dim) by default; lse (float32 [tokens, heads]) is
     filled if given.  Returns out [tokens, heads, head_dim]."""
-    dtype = _type_of(q, "q")
+    code, dtype = _type_of(q, "q"), q.dtype
     if plan.kv_len is None:
         raise ValueError("plan: make() it for the batch first")
-    n_req, T, Hq, H, D, max_new = plan.args
+    _, T, Hq, H, D, max_new = plan.args
     if H != cache.n_kv_heads or D != cache.head_dim:
         raise ValueError("plan and cache differ in heads or head_dim")
-    batch = _batch(page_table, plan.q_off, plan.kv_len, T)
     out = _new(q) if out is None else out
-    if lse is not None and tuple(lse.shape) != (T, Hq):
+    if lse is not None and lse.shape != (T, Hq):
         raise ValueError(f"lse: expected shape {(T, Hq)}")
-    a, b = _heads(q, q.dtype, (T, Hq, D), "q"), _heads(out, q.dtype, (T, Hq, D), "out")
+    shape = (T, Hq, D)
     _check("smetric_attend", _lib.smetric_attend(
-        dtype, cache.ref, C.addressof(batch), Hq, C.addressof(a), C.addressof(b), _opt(lse, torch.float32, "lse"),
-        1.0 / math.sqrt(D) if scale is None else scale, max_new, plan.window, plan.mem.data_ptr(), plan.plan_bytes,
-        plan.workspace.data_ptr(), plan.ws_bytes, _opt(status, torch.int32, "status"), _stream()))
+        code, cache.ref, _batch(page_table, plan.q_off, plan.kv_len, T), Hq, _heads(q, dtype, shape, "q"),
+        _heads(out, dtype, shape, "out"), _opt(lse, torch.float32, "lse"), D ** -0.5 if scale is None else scale, max_new,
+        plan.window, plan.plan_ptr, plan.plan_bytes, plan.ws_ptr, plan.ws_bytes, _opt(status, torch.int32, "status"),
+        _stream()))
     return out
