@@ -29,11 +29,23 @@ __device__ __forceinline__ u32x2 swap32(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
 }
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void global_void;
-// 64 lanes' 16 bytes from memory to 1 KB of LDS, past the registers.
-__device__ __forceinline__ void to_lds(const char *from, char *to) {
-  __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
+// 64 lanes' 16 bytes from memory to 1 KB of LDS, past the registers.  The instruction has no
+// output the compiler could take for written; what waits for it is arrived().  (With the
+// compiler's builtin, every later read of LDS waits for it, since both buffers are one
+// array to the alias analysis.)
+__device__ __forceinline__ void to_lds(uint64_t base, uint32_t offset, char *to) {
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)to));
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void to_lds(uint64_t from, char *to) {
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)to));
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from)
+               : "memory", "m0");
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {  // one instruction; NaN stays
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
@@ -53,27 +65,26 @@ struct Rows {
   int32_t hi, lo;    // the keys [lo, hi) that the row sees
 };
 
-// One step's 64 keys.  MASKED: some row does not see all of them; odd: and some value is not
-// finite.
+// One step's 64 keys: the scores.  S^T: lane (half, col) gets row col's scores of keys kb +
+// 32 j + 8 (r / 4) + 4 half + r % 4, -inf for those that the row does not see (MASKED: there
+// may be some).  Returns the row's largest.
 template <typename T, int D, bool MASKED>
-__device__ __forceinline__ void step(Rows<D> &w, const char (&kl)[KT * 2 * D], const char (&vl)[KT * 2 * D], int32_t kb,
-                                     float sc, bool odd, int lane) {
-  constexpr int STEPS = D / 16, DT = D / 32, ROWB = 2 * D;
-  constexpr int KSW = D == 64 ? 7 : 15, VSW = D == 64 ? 3 : 7;
+__device__ __forceinline__ float scores(const Rows<D> &w, const char *kl, int32_t kb, float sc, int lane,
+                                        f32x16 (&s)[2]) {
+  constexpr int STEPS = D / 16, ROWB = 2 * D, KSW = D == 64 ? 7 : 15;
   const int col = lane & 31, half = lane >> 5;
-  // S^T: lane (half, col) gets row col's scores of keys kb + 32 j + 8 (r / 4) + 4 half + r % 4
-  f32x16 s[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
 #pragma unroll
-    for (int t = 0; t < STEPS; ++t) {
+  for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
       const int kr = 32 * j + col;
       const u32x4 k = *reinterpret_cast<const u32x4 *>(kl + kr * ROWB + (((2 * t + half) ^ (kr & KSW)) * 16));
       s[j] = T::mfma32(k, w.q[t], s[j]);
     }
-  }
   if (MASKED) {
     const int32_t hi = w.hi - kb - 4 * half, lo = w.lo - kb - 4 * half;
 #pragma unroll
@@ -91,65 +102,115 @@ __device__ __forceinline__ void step(Rows<D> &w, const char (&kl)[KT * 2 * D], c
   for (int r = 1; r < 15; r += 2) mx = max3(mx, s[1][r], s[1][r + 1]);
   mx = __builtin_elementwise_maximum(mx, s[1][15]);
   const u32x2 both = swap32(__float_as_uint(mx), __float_as_uint(mx));
-  mx = __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * sc;
-  while (__any(mx > w.m + SLACK)) {  // at most once, and at first: m is -inf.  A loop, so that the sums stay in place
-    const float mn = fmaxf(w.m, mx);
-    const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
-    w.m = mn;
-    w.l *= down;
-#pragma unroll
-    for (int i = 0; i < DT; ++i) w.o[i] *= down;
-  }
-  const float base = T::P_SHIFT - (w.m == -INFINITY ? 0.0f : w.m);
-  float l0 = 0.0f, l1 = 0.0f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], sc, base));
-    s[1][r] = __builtin_amdgcn_exp2f(fmaf(s[1][r], sc, base));
-    l0 += s[0][r];
-    l1 += s[1][r];
-  }
-  w.l += l0 + l1;
-  if (MASKED && odd) {
-    // some value is not finite and rows differ in what they see: 0 times it must not reach a
-    // row that does not see it.  Rare, so plain sums: weight r of either half.
-#pragma unroll 1
-    for (int r = 0; r < 32; ++r) {
-#pragma unroll 1
-      for (int h = 0; h < 2; ++h) {
-        const float p = __shfl(s[0][0], col + 32 * h);
-        const int vrow = 32 * (r / 16) + 8 * (r % 16 / 4) + 4 * h + r % 4, key = kb + vrow;
-        const bool seen = key < w.hi && key >= w.lo;
-#pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {  // components 32 i + 8 g + 4 half + 0 .. 3
-            const u32x2 x = *reinterpret_cast<const u32x2 *>(vl + vrow * ROWB + (((4 * i + g) ^ (2 * (vrow & VSW))) * 16) +
-                                                             half * 8);
-            const float v[4] = {T::lo(x.x), T::hi(x.x), T::lo(x.y), T::hi(x.y)};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w.o[i][4 * g + k] = seen ? fmaf(p, v[k], w.o[i][4 * g + k]) : w.o[i][4 * g + k];
-          }
-      }
-#pragma unroll
-      for (int k = 0; k < 31; ++k) s[k / 16][k % 16] = s[(k + 1) / 16][(k + 1) % 16];
-    }
-    return;
-  }
+  return __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * sc;
+}
+template <typename T, int D>
+__device__ __forceinline__ float exponent(const Rows<D> &w) {  // of weight 2^P_SHIFT
+  return T::P_SHIFT - (w.m == -INFINITY ? 0.0f : w.m);
+}
+
+// The weights, 16 keys' at a time, and the products of the 16 before them with their values.
+template <typename T, int D>
+__device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, int lane,
+                                         const f32x16 (&s)[2]) {
+  constexpr int DT = D / 32, ROWB = 2 * D, VSW = D == 64 ? 3 : 7;
+  const int half = lane >> 5, j = lane & 15;
+  const float base = exponent<T>(w);
 #pragma unroll
   for (int t = 0; t < KT / 16; ++t) {
     u32x4 p;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) p[e] = T::pack(s[t / 2][8 * (t % 2) + 2 * e], s[t / 2][8 * (t % 2) + 2 * e + 1]);
+    for (int e = 0; e < 4; ++e) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e], sc, base));
+      const float y = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e + 1], sc, base));
+      w.l += x + y;
+      p[e] = T::pack(x, y);
+    }
 #pragma unroll
     for (int i = 0; i < DT; ++i) {
-      const int j = lane & 15;
       const int r = 16 * t + 4 * half + j / 4, c = 4 * i + 2 * ((lane >> 4) & 1) + (j % 4) / 2;
       const u32x2 v0 = read_transposed(vl + r * ROWB + ((c ^ (2 * (r & VSW))) * 16) + (j & 1) * 8);
       const u32x2 v1 = read_transposed(vl + (r + 8) * ROWB + ((c ^ (2 * ((r + 8) & VSW))) * 16) + (j & 1) * 8);
       w.o[i] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p, w.o[i]);
     }
   }
+}
+
+// The products where some value is not finite and rows differ in what they see: 0 times it
+// must not reach a row that does not see it.  Rare, so plain sums: weight r of either half.
+template <typename T, int D>
+__device__ __forceinline__ void products_apart(Rows<D> &w, const char *vl, int32_t kb, float sc, int lane,
+                                               f32x16 (&s)[2]) {
+  constexpr int DT = D / 32, ROWB = 2 * D, VSW = D == 64 ? 3 : 7;
+  const int col = lane & 31, half = lane >> 5;
+  const float base = exponent<T>(w);
+  float pair = 0.0f;
+#pragma unroll 1
+  for (int r = 0; r < 32; ++r) {
+    const float x = __builtin_amdgcn_exp2f(fmaf(s[0][0], sc, base));
+    if (r % 2) w.l += pair + x;  // in the order of products()
+    pair = x;
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+      const float p = __shfl(x, col + 32 * h);
+      const int vrow = 32 * (r / 16) + 8 * (r % 16 / 4) + 4 * h + r % 4, key = kb + vrow;
+      const bool seen = key < w.hi && key >= w.lo;
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {  // components 32 i + 8 g + 4 half + 0 .. 3
+          const u32x2 x2 = *reinterpret_cast<const u32x2 *>(vl + vrow * ROWB + (((4 * i + g) ^ (2 * (vrow & VSW))) * 16) +
+                                                            half * 8);
+          const float v[4] = {T::lo(x2.x), T::hi(x2.x), T::lo(x2.y), T::hi(x2.y)};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w.o[i][4 * g + k] = seen ? fmaf(p, v[k], w.o[i][4 * g + k]) : w.o[i][4 * g + k];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 31; ++k) s[k / 16][k % 16] = s[(k + 1) / 16][(k + 1) % 16];
+  }
+}
+
+// Where some row's maximum has grown by more than 2^SLACK: sums scaled down.  The branch
+// around the products is part of the instruction sequence, so that for the compiler the sums
+// are changed in one place and keep their registers; around a branch of its own it keeps
+// them twice, which leaves no room for keys and values read ahead.  The products of the
+// step before are long done: this step's scores, which came after them, have been read.
+__device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown) {
+  float x[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = o[r];
+  asm volatile(
+      "s_cmp_eq_u64 %17, 0\n\ts_cbranch_scc1 .Lkept%=\n\t"
+      "v_mul_f32 %0, %16, %0\n\tv_mul_f32 %1, %16, %1\n\tv_mul_f32 %2, %16, %2\n\tv_mul_f32 %3, %16, %3\n\t"
+      "v_mul_f32 %4, %16, %4\n\tv_mul_f32 %5, %16, %5\n\tv_mul_f32 %6, %16, %6\n\tv_mul_f32 %7, %16, %7\n\t"
+      "v_mul_f32 %8, %16, %8\n\tv_mul_f32 %9, %16, %9\n\tv_mul_f32 %10, %16, %10\n\tv_mul_f32 %11, %16, %11\n\t"
+      "v_mul_f32 %12, %16, %12\n\tv_mul_f32 %13, %16, %13\n\tv_mul_f32 %14, %16, %14\n\tv_mul_f32 %15, %16, %15\n"
+      ".Lkept%=:"
+      : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]), "+v"(x[8]),
+        "+v"(x[9]), "+v"(x[10]), "+v"(x[11]), "+v"(x[12]), "+v"(x[13]), "+v"(x[14]), "+v"(x[15])
+      : "v"(down), "s"(grown)
+      : "scc");
+#pragma unroll
+  for (int r = 0; r < 16; ++r) o[r] = x[r];
+}
+
+// A step.  ENDS: not every row sees all of its keys; odd: and some value is not finite.
+template <typename T, int D, bool ENDS>
+__device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc, bool odd, int lane) {
+  f32x16 s[2];
+  const float mx = scores<T, D, ENDS>(w, kl, kb, sc, lane, s);
+  const uint64_t grown = __ballot(mx > w.m + SLACK);  // also the first time: m is -inf
+  const float mn = grown ? fmaxf(w.m, mx) : w.m;
+  const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
+  w.m = mn;
+  w.l *= down;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
+  if (ENDS && odd)
+    products_apart<T>(w, vl, kb, sc, lane, s);
+  else
+    products<T>(w, vl, sc, lane, s);
 }
 
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
@@ -163,11 +224,8 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
   constexpr int STEPS = D / 16, DT = D / 32;
   constexpr int ROWB = 2 * D;         // bytes of a row in LDS
   constexpr int KSW = D == 64 ? 7 : 15, VSW = D == 64 ? 3 : 7;  // exchange of 16-byte pieces within a row
-  // four arrays, so that the compiler sees that loads into one do not change the others
-  __shared__ __attribute__((aligned(1024))) char k_even[KT * ROWB];
-  __shared__ __attribute__((aligned(1024))) char k_odd[KT * ROWB];
-  __shared__ __attribute__((aligned(1024))) char v_even[KT * ROWB];
-  __shared__ __attribute__((aligned(1024))) char v_odd[KT * ROWB];
+  constexpr int SIDE = KT * ROWB;     // bytes of a step's keys, and of its values
+  __shared__ __attribute__((aligned(1024))) char lds[4 * SIDE];  // a step's keys, values; the next one's
   __shared__ int32_t odd_step;  // the last step with a value that is not finite
 
   const int32_t kvh = blockIdx.x % a.n_kv, share = blockIdx.x / a.n_kv;
@@ -253,7 +311,8 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
     const uint32_t k_lane = uint32_t(lrow) * uint32_t(a.cache.k.token), v_lane = uint32_t(lrow) * uint32_t(a.cache.v.token);
     // From memory: 16-bit rows straight to LDS, each lane fetching the piece that belongs where
     // its 16 bytes land; 8-bit ones to registers, from which to_16 widens them.
-    const auto load_step = [&](int32_t kb, char *kl, char *vl) {
+    const auto load_step = [&](int32_t kb, char *kl) {
+      char *vl = kl + SIDE;
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int r = i * RPL + wave * RPW;  // the wavefront's first row
@@ -261,29 +320,31 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
         uint64_t kp, vp;
         uint32_t ko = kc * 16, vo = vc * 16;
         if (WIDE) {
-          const int from = int(uint32_t(kb - known_from + r) / 16);
+          const int from = (kb - known_from + r) / 16;
           kp = read_lane(kp_l, from);
           vp = read_lane(vp_l, from);
           ko += k_lane + uint32_t(r % 16) * uint32_t(a.cache.k.token);
           vo += v_lane + uint32_t(r % 16) * uint32_t(a.cache.v.token);
-        asm("" : "+v"(ko), "+v"(vo));  // stays a 32-bit offset to a scalar address
         } else {
           int32_t key = kb + r + lrow;
           key = key < last_key ? key : last_key;
           key = key > k0 ? key : k0;
           find(key, kp, vp);
         }
-        const char *k = reinterpret_cast<const char *>(kp) + ko, *v = reinterpret_cast<const char *>(vp) + vo;
         if (KV8) {
-          kr[i] = *reinterpret_cast<const u32x4 *>(k);
-          vr[i] = *reinterpret_cast<const u32x4 *>(v);
+          kr[i] = *reinterpret_cast<const u32x4 *>(kp + ko);
+          vr[i] = *reinterpret_cast<const u32x4 *>(vp + vo);
+        } else if (WIDE) {
+          to_lds(kp, ko, kl + r * ROWB);
+          to_lds(vp, vo, vl + r * ROWB);
         } else {
-          to_lds(k, kl + r * ROWB);
-          to_lds(v, vl + r * ROWB);
+          to_lds(kp + ko, kl + r * ROWB);
+          to_lds(vp + vo, vl + r * ROWB);
         }
       }
     };
-    const auto to_16 = [&](char *kl, char *vl) {
+    const auto to_16 = [&](char *kl) {
+      char *vl = kl + SIDE;
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int r = i * RPL + wave * RPW + lrow;
@@ -322,39 +383,42 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
     };
-    // One step: the next one's loads, this one's products.  ENDS: some row of the tile does not
-    // see all of its keys.
-    const auto turn = [&](auto ends, int32_t kb, char(&kl)[KT * ROWB], char(&vl)[KT * ROWB], char *k_next, char *v_next) {
-      constexpr bool ENDS = decltype(ends)::value;
+    int buf = 0;  // where the current step's keys and values are
+    const auto here = [&] { return lds + buf * (2 * SIDE); };
+    const auto there = [&] { return lds + (buf ^ 1) * (2 * SIDE); };
+    const auto load_next = [&](int32_t kb) {
       const int32_t next = kb + KT;
-      if (next < k1) {
-        if (WIDE && next - known_from >= 64 * 16) find_steps(next);
-        load_step(next, k_next, v_next);
+      if (next >= k1) return;
+      if (WIDE && next - known_from >= 64 * 16) find_steps(next);
+      load_step(next, there());
+    };
+    // Steps from kb to `to`.  ENDS: not every row of the tile sees all of their keys.  Every
+    // wavefront passes the same barriers: one a step, and those of look_over.
+    const auto run = [&](auto ends, int32_t &kb, int32_t to) {
+      constexpr bool ENDS = decltype(ends)::value;
+      for (; kb < to; kb += KT, buf ^= 1) {
+        load_next(kb);
+        if (ENDS) look_over(kb, here() + SIDE);
+        if (!ENDS || (n_rows > 0 && kb < max_hi && kb + KT > min_lo))
+          step<T, D, ENDS>(w, here(), here() + SIDE, kb, sc, ENDS && odd_step == kb, lane);
+        if (KV8 && kb + KT < k1) to_16(there());
+        arrived();
       }
-      if (ENDS) look_over(kb, vl);
-      if (!ENDS || (kb < max_hi && kb + KT > min_lo)) step<T, D, ENDS>(w, kl, vl, kb, sc, ENDS && odd_step == kb, lane);
-      if (KV8 && next < k1) to_16(k_next, v_next);
-      arrived();
     };
 
     __syncthreads();  // odd_step is set before a step may mark it
     if (kb0 < k1) {
-      // steps that every row sees whole; the others, and a lone one beside them, take the other form
-      const int32_t full0 = (max(k0, tile_max_lo) + KT - 1) / KT * KT, full1 = min(k1, tile_min_hi);
+      // steps that every row of the tile sees whole lie between full0 and full1
+      const int32_t full0 = (max(k0, tile_max_lo) + KT - 1) / KT * KT, full1 = min(k1, tile_min_hi) / KT * KT;
       if (WIDE) find_steps(kb0);
-      load_step(kb0, k_even, v_even);
-      if (KV8) to_16(k_even, v_even);
+      load_step(kb0, here());
+      if (KV8) to_16(here());
       arrived();
       int32_t kb = kb0;
-      while (kb < k1) {
-        for (; kb >= full0 && kb + 2 * KT <= full1; kb += 2 * KT) {
-          turn(std::false_type{}, kb, k_even, v_even, k_odd, v_odd);
-          turn(std::false_type{}, kb + KT, k_odd, v_odd, k_even, v_even);
-        }
-        if (kb < k1) turn(std::true_type{}, kb, k_even, v_even, k_odd, v_odd);
-        kb += KT;
-        if (kb < k1) turn(std::true_type{}, kb, k_odd, v_odd, k_even, v_even);
-        kb += KT;
+#pragma unroll 1
+      for (int part = 0; part < 2; ++part) {
+        run(std::true_type{}, kb, part ? k1 : min(full0, k1));
+        if (!part) run(std::false_type{}, kb, full1);
       }
     }
     if (bad_page) set_status(a.status, SMETRIC_EINVAL);
