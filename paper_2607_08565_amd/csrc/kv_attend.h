@@ -40,9 +40,12 @@ static_assert(sizeof(PlanHdr) == 128 && sizeof(PlanItem) == 32 && sizeof(PlanSpl
 // compute units), each with an equal share of the key steps in order, so that all end
 // together; a share begins and ends within a tile, which is then in pieces, and may hold
 // several tiles.  Two exceptions: no share is smaller than MIN_STEPS, and a cut this near a
-// tile's end goes to the end (EDGE_STEPS).
+// tile's end goes to the end (EDGE_STEPS).  Few rows: a step is half a block of each
+// wavefront, so two make the shortest share that occupies all four (one token over 1,025 keys:
+// 5.8 us, with shares of four steps 8.3, of eight 11.6).
 constexpr int32_t TARGET = 512;
-constexpr int32_t FEW_MIN_STEPS = 4, MANY_MIN_STEPS = 8, FEW_EDGE_STEPS = 2, MANY_EDGE_STEPS = 4;
+constexpr int32_t FEW_MIN_STEPS = 2, FEW_EDGE_STEPS = 1, FEW_TILE_COST = 0;
+constexpr int32_t MANY_MIN_STEPS = 8, MANY_EDGE_STEPS = 4, MANY_TILE_COST = 2;
 
 struct PlanShape {
   int32_t rows, target;  // rows per tile; workgroups aimed at per key-value head

@@ -13,13 +13,12 @@ namespace {
 
 constexpr int PT = 512;
 constexpr int32_t STAGED = 2048;   // requests whose offsets and lengths are kept in LDS
-constexpr int32_t TILE_COST = 2;   // steps: a tile's queries, first pages and output
 constexpr int32_t CUT_COST = 12;   // steps: what a share's partial results cost, see whole_tiles
 
 struct PlanArgs {
   const int64_t *q_off;
   const int32_t *kv_len;
-  int32_t n_req, n_q, n_kv, group, rows, rows_log2, window, target, min_steps, edge_steps;
+  int32_t n_req, n_q, n_kv, group, rows, rows_log2, window, target, min_steps, edge_steps, tile_cost;
   int64_t n_tokens, max_tiles, max_items, max_groups, max_splits, max_parts;
   PlanHdr *hdr;
   PlanItem *items;
@@ -59,6 +58,11 @@ __device__ Tile tile_at(const PlanArgs &a, const int64_t *q_off, const int32_t *
   if (t.k1 <= t.k0) t.k0 = t.k1 = 0;
   t.steps = (t.k1 + KEY_STEP - 1) / KEY_STEP - t.k0 / KEY_STEP;
   return t;
+}
+
+// A tile's steps, and what it costs besides (its queries, first pages and output), in steps.
+__device__ __forceinline__ int32_t cost_of(const PlanArgs &a, const Tile &t) {
+  return (t.steps > 0 ? t.steps : 1) + a.tile_cost;
 }
 
 // floor(x / d) for 0 <= x < 2^52: a quotient in 64-bit floats is at most one off.
@@ -138,7 +142,7 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
     for (int64_t g = threadIdx.x; g < a.max_tiles; g += PT) {
       t = tile_at(a, q_off, kv_len, g);
       if (t.req < 0) continue;
-      const int32_t c = t.steps + TILE_COST;
+      const int32_t c = cost_of(a, t);
       mine += c;
       top = c > top ? c : top;
       ++count;
@@ -147,20 +151,20 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
     int64_t cost, tiles;
     scan<int64_t>(mine, cost, sh64);
     scan<int64_t>(count, tiles, sh64);
-    const int32_t least = a.min_steps + TILE_COST;
+    const int32_t least = a.min_steps + a.tile_cost;
     int64_t groups = quotient(cost + least - 1, least);
     if (groups > a.target) groups = a.target;
     if (groups < 1) groups = 1;
     const int64_t share = cost > 0 ? quotient(cost + groups - 1, groups) : 1;
     const bool whole = whole_tiles(cost, tiles, longest, a.target);
     n_groups = whole ? tiles : quotient(cost + share - 1, share);
-    const int32_t edge = a.edge_steps + TILE_COST;
+    const int32_t edge = a.edge_steps + a.tile_cost;
     int64_t at0 = 0;
     for (int64_t g0 = 0; g0 < a.max_tiles; g0 += PT) {
       const int64_t g = g0 + threadIdx.x;
       if (a.max_tiles > PT || g >= a.max_tiles) t.req = -1;
       if (a.max_tiles > PT && g < a.max_tiles) t = tile_at(a, q_off, kv_len, g);
-      const int64_t c = t.req < 0 ? 0 : t.steps + TILE_COST;
+      const int64_t c = t.req < 0 ? 0 : cost_of(a, t);
       int64_t all;
       const int64_t at = at0 + scan<int64_t>(c, all, sh64);
       at0 += all;
@@ -178,8 +182,8 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
       const int64_t split_at = n_splits + scan<int32_t>(cuts > 0, all_s, sh32);
       const int32_t k = t.k0 / KEY_STEP;
       for (int32_t i = 0; i < pieces && base + i < a.max_items; ++i) {
-        const int32_t c0 = i ? int32_t((w_lo + i - 1) * share - at) - TILE_COST : 0;
-        const int32_t c1 = i < cuts ? int32_t((w_lo + i) * share - at) - TILE_COST : 0;
+        const int32_t c0 = i ? int32_t((w_lo + i - 1) * share - at) - a.tile_cost : 0;
+        const int32_t c1 = i < cuts ? int32_t((w_lo + i) * share - at) - a.tile_cost : 0;
         a.items[base + i] = PlanItem{t.req, t.tok0, t.n_new, t.kv_len, t.tile, i == 0 ? t.k0 : (k + c0) * KEY_STEP,
                                      i == cuts ? t.k1 : (k + c1) * KEY_STEP, cuts ? int32_t(part0 + i) : -1};
       }
@@ -336,6 +340,7 @@ extern "C" int smetric_attend_plan(const int64_t *q_off, const int32_t *kv_len, 
   char *p = static_cast<char *>(plan);
   PlanArgs a{q_off, kv_len, n_req, n_q_heads, n_kv_heads, n_q_heads / n_kv_heads, s.rows, s.rows == FEW_ROWS ? 4 : 7, window, s.target,
              s.rows == FEW_ROWS ? FEW_MIN_STEPS : MANY_MIN_STEPS, s.rows == FEW_ROWS ? FEW_EDGE_STEPS : MANY_EDGE_STEPS,
+             s.rows == FEW_ROWS ? FEW_TILE_COST : MANY_TILE_COST,
              n_tokens, n_req ? s.max_tiles : 0, s.max_items, s.max_groups, s.max_splits, s.max_parts,
              reinterpret_cast<PlanHdr *>(p), reinterpret_cast<PlanItem *>(p + s.off_items),
              reinterpret_cast<PlanSplit *>(p + s.off_splits), reinterpret_cast<int32_t *>(p + s.off_first), status};

@@ -100,6 +100,22 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
   const int kind = h < n_q ? 0 : h < n_q + n_kv ? 1 : 2;
   const int32_t head = kind == 0 ? h : kind == 1 ? h - n_q : h - n_q - n_kv;
 
+  // this lane's two pieces of 8 components
+  const int half = ta.rot / 16;
+  int c0 = sub, c1 = sub + LPR;
+  if (!INTER) {
+    c0 = sub < half ? sub : 2 * sub;
+    c1 = sub < half ? sub + half : 2 * sub + 1;
+  }
+  // (which of the two turn: both or none for halves)
+  const bool turns0 = c0 < (INTER ? 2 * half : half) && kind != 2;
+  const bool turns1 = INTER ? c1 < 2 * half && kind != 2 : turns0;
+  // asked for before the chain of loads that finds the place
+  const HeadsView &src = kind == 0 ? q : kind == 1 ? k : v;
+  const uint16_t *from = src.data + t * src.token + head * src.head;
+  const u32x4 in0 = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + 8 * c0));
+  const u32x4 in1 = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + 8 * c1));
+
   int32_t place = 0, pos = 0;
   int64_t page_row = 0;
   bool ok = live, bad = false;
@@ -131,24 +147,9 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
   }
   if (live && bad && sub == 0) set_status(ta.status, SMETRIC_EINVAL);
 
-  // this lane's two pieces of 8 components
-  const int half = ta.rot / 16;
-  int c0 = 2 * sub, c1 = 2 * sub + 1;
-  if (!INTER && sub < half) {
-    c0 = sub;
-    c1 = sub + half;
-  }
-  const bool turns = sub < half && kind != 2;
   float x[16];
-  const HeadsView &src = kind == 0 ? q : kind == 1 ? k : v;
-  if (ok) {
-    const uint16_t *p = src.data + t * src.token + head * src.head;
-    widen<T>(*reinterpret_cast<const u32x4 *>(p + 8 * c0), x);
-    widen<T>(*reinterpret_cast<const u32x4 *>(p + 8 * c1), x + 8);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-  }
+  widen<T>(ok ? in0 : u32x4{0, 0, 0, 0}, x);
+  widen<T>(ok ? in1 : u32x4{0, 0, 0, 0}, x + 8);
   const uint16_t *w = static_cast<const uint16_t *>(kind == 2 ? nullptr : ta.weight[kind]);
   // the exchange is outside the condition: rows with and without a weight share a wavefront
   float ss = 0.0f;
@@ -164,13 +165,17 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = x[i] * rstd * g[i];
   }
-  if (turns && ok) {
-    const float *cs = ta.table + int64_t(pos) * ta.rot + 8 * sub;
-    const float *sn = cs + ta.rot / 2;
+  if (ok && (turns0 || turns1)) {
+    // angles: eight in a row for halves; four of each piece for neighbours
+    const float *cs = ta.table + int64_t(pos) * ta.rot, *sn = cs + ta.rot / 2;
+    const int a0 = INTER ? 4 * c0 : 8 * sub, a1 = INTER ? 4 * c1 : 8 * sub + 4;
     float co[8], si[8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const f32x4 a = *reinterpret_cast<const f32x4 *>(cs + 4 * i), b = *reinterpret_cast<const f32x4 *>(sn + 4 * i);
+      const bool on = i ? turns1 : turns0;
+      const int at = i ? a1 : a0;
+      const f32x4 a = on ? *reinterpret_cast<const f32x4 *>(cs + at) : f32x4{1, 1, 1, 1};
+      const f32x4 b = on ? *reinterpret_cast<const f32x4 *>(sn + at) : f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         co[4 * i + j] = a[j];
@@ -179,6 +184,7 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+      if (INTER && !(i < 4 ? turns0 : turns1)) continue;
       float &a = INTER ? x[2 * i] : x[i], &b = INTER ? x[2 * i + 1] : x[8 + i];
       const float ya = a, yb = b;
       a = ya * co[i] - yb * si[i];
@@ -202,8 +208,13 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
   } else {
     const HeadsView &dst = kind == 0 ? q_out : k_out;
     uint16_t *p = dst.data + t * dst.token + head * dst.head;
-    *reinterpret_cast<u32x4 *>(p + 8 * c0) = narrow<T>(x);
-    *reinterpret_cast<u32x4 *>(p + 8 * c1) = narrow<T>(x + 8);
+    if (PAGED) {  // attention reads it next
+      *reinterpret_cast<u32x4 *>(p + 8 * c0) = narrow<T>(x);
+      *reinterpret_cast<u32x4 *>(p + 8 * c1) = narrow<T>(x + 8);
+    } else {
+      __builtin_nontemporal_store(narrow<T>(x), reinterpret_cast<u32x4 *>(p + 8 * c0));
+      __builtin_nontemporal_store(narrow<T>(x + 8), reinterpret_cast<u32x4 *>(p + 8 * c1));
+    }
   }
 }
 
