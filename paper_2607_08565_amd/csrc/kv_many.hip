@@ -32,17 +32,20 @@ __device__ __forceinline__ u32x2 swap32(uint32_t a, uint32_t b) {
 // 64 lanes' 16 bytes from memory to 1 KB of LDS, past the registers.  The instruction has no
 // output the compiler could take for written; what waits for it is arrived().  (With the
 // compiler's builtin, every later read of LDS waits for it, since both buffers are one
-// array to the alias analysis.)
+// array to the alias analysis.)  The waits are those that the hardware leaves to the program,
+// where the compiler does not see into these lines: one instruction between the write of M0
+// and the load, and five between a vector instruction that writes a scalar register, as
+// read_lane does, and a load that reads it.
 __device__ __forceinline__ void to_lds(uint64_t base, uint32_t offset, char *to) {
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)to));
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base)
                : "memory", "m0");
 }
 __device__ __forceinline__ void to_lds(uint64_t from, char *to) {
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)to));
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :
                : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from)
                : "memory", "m0");
@@ -175,7 +178,8 @@ __device__ __forceinline__ void products_apart(Rows<D> &w, const char *vl, int32
 // around the products is part of the instruction sequence, so that for the compiler the sums
 // are changed in one place and keep their registers; around a branch of its own it keeps
 // them twice, which leaves no room for keys and values read ahead.  The products of the
-// step before are long done: this step's scores, which came after them, have been read.
+// step before are long done: this step's scores, which came after them, have been read.  The
+// next product may read what was scaled two instructions later, hence the wait at the end.
 __device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown) {
   float x[16];
 #pragma unroll
@@ -185,7 +189,8 @@ __device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown
       "v_mul_f32 %0, %16, %0\n\tv_mul_f32 %1, %16, %1\n\tv_mul_f32 %2, %16, %2\n\tv_mul_f32 %3, %16, %3\n\t"
       "v_mul_f32 %4, %16, %4\n\tv_mul_f32 %5, %16, %5\n\tv_mul_f32 %6, %16, %6\n\tv_mul_f32 %7, %16, %7\n\t"
       "v_mul_f32 %8, %16, %8\n\tv_mul_f32 %9, %16, %9\n\tv_mul_f32 %10, %16, %10\n\tv_mul_f32 %11, %16, %11\n\t"
-      "v_mul_f32 %12, %16, %12\n\tv_mul_f32 %13, %16, %13\n\tv_mul_f32 %14, %16, %14\n\tv_mul_f32 %15, %16, %15\n"
+      "v_mul_f32 %12, %16, %12\n\tv_mul_f32 %13, %16, %13\n\tv_mul_f32 %14, %16, %14\n\tv_mul_f32 %15, %16, %15\n\t"
+      "s_nop 1\n"
       ".Lkept%=:"
       : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]), "+v"(x[8]),
         "+v"(x[9]), "+v"(x[10]), "+v"(x[11]), "+v"(x[12]), "+v"(x[13]), "+v"(x[14]), "+v"(x[15])
