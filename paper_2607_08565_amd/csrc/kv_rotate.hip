@@ -157,7 +157,7 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
   for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
   for (int m = 1; m < LPR; m *= 2) ss += __shfl_xor(ss, m, 64);
-  if (w) {
+  if (w && ok) {  // (zeros stay zeros also where eps is 0)
     const float rstd = 1.0f / sqrtf(ss * (1.0f / D) + ta.eps);
     float g[16];
     widen<T>(*reinterpret_cast<const u32x4 *>(w + 8 * c0), g);

@@ -182,6 +182,22 @@ def test_append_bad_inputs_write_nothing():
         assert bool((q[0] == 0).all()) and bool((q[1] == 1).all())
 
 
+def test_padding_is_zeros_without_eps():
+    """Where eps is 0 a token of zeros has no norm; what padding and bad positions leave is zeros all the same."""
+    kv = _kv()
+    D = 64
+    w = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    r = kv.Rotary(table_of(8, D).cuda(), q_weight=w, k_weight=w, eps=0.0)
+    x = torch.ones(2, 3, D, dtype=torch.bfloat16, device="cuda")
+    z = torch.zeros(1, 1, 16, D, dtype=torch.bfloat16, device="cuda")
+    c = kv.PagedCache(z, z.clone())
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    q = kv.append(c, i32(0, 0)[:, None], torch.tensor([0, 1, 2], device="cuda"), i32(0, 1), x[:, :1], x[:, 1:2], q=x, rotary=r)
+    assert bool((q[0] == 0).all()) and bool((q[1] == 1).all())
+    a, b = kv.qk_rotate(x, x[:, :1], r, i32(8, 0))
+    assert bool((a[0] == 0).all()) and bool((b[0] == 0).all()) and bool((a[1] == 1).all()) and bool((b[1] == 1).all())
+
+
 def test_refusals():
     kv = _kv()
     from paper_2607_08565_amd.smetric import SmetricError
