@@ -309,6 +309,9 @@ int launch_join(const AttendArgs &a, int32_t head_dim, int64_t max_splits, hipSt
                         : head_dim == 128 ? launch_join_d<T, 128>(a, max_splits, stream) : launch_join_d<T, 256>(a, max_splits, stream);
 }
 
+// A window of all places is none: what the kernels subtract from a place stays in 32 bits.
+int32_t window_of(int32_t window) { return window >= MAX_PLACES ? 0 : window; }
+
 bool shape_ok(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t max_new) {
   return n_req >= 0 && n_tokens >= 0 && (n_req > 0 || n_tokens == 0) && n_kv >= 1 && n_q >= n_kv && n_q <= 65536 &&
          n_q % n_kv == 0 && n_tokens * (n_q / n_kv) < 0x7FFFFFFF && n_tokens <= 0x7FFFFFFF && max_new >= 1 &&
@@ -338,7 +341,7 @@ extern "C" int smetric_attend_plan(const int64_t *q_off, const int32_t *kv_len, 
   const PlanShape s = plan_shape(n_req, n_tokens, n_q_heads, n_kv_heads, head_dim, max_new);
   if (plan_bytes < s.plan_bytes) return SMETRIC_EWORKSPACE;
   char *p = static_cast<char *>(plan);
-  PlanArgs a{q_off, kv_len, n_req, n_q_heads, n_kv_heads, n_q_heads / n_kv_heads, s.rows, s.rows == FEW_ROWS ? 4 : 7, window, s.target,
+  PlanArgs a{q_off, kv_len, n_req, n_q_heads, n_kv_heads, n_q_heads / n_kv_heads, s.rows, s.rows == FEW_ROWS ? 4 : 7, window_of(window), s.target,
              s.rows == FEW_ROWS ? FEW_MIN_STEPS : MANY_MIN_STEPS, s.rows == FEW_ROWS ? FEW_EDGE_STEPS : MANY_EDGE_STEPS,
              s.rows == FEW_ROWS ? FEW_TILE_COST : MANY_TILE_COST,
              n_tokens, n_req ? s.max_tiles : 0, s.max_items, s.max_groups, s.max_splits, s.max_parts,
@@ -382,7 +385,7 @@ extern "C" int smetric_attend(int32_t dtype, const smetric_kv_cache *cache, cons
   a.n_kv = cache->n_kv_heads;
   a.group = n_q_heads / cache->n_kv_heads;
   a.rows = s.rows;
-  a.window = window;
+  a.window = window_of(window);
   a.scale_log2 = scale * 1.4426950408889634f;
   a.status = status;
   const bool kv8 = cache->dtype == SMETRIC_E4M3;

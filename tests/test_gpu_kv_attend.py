@@ -107,6 +107,17 @@ def test_pages_and_windows(page, order, fp8, window):
     Case([(3, 3), (90, 40), (2, 3), (200, 1), (140, 77), (500, 33)], 8, 2, 128, BF, fp8, page, order, window, seed=4).check()
 
 
+@pytest.mark.parametrize("window", [(1 << 24) - 1, 1 << 24, (1 << 31) - 1])
+@pytest.mark.parametrize("max_new", [1, 1000])
+def test_windows_longer_than_any_request(window, max_new):
+    """Also for tokens whose place is negative."""
+    lens = [(2, 5), (0, 3), (3, 40), (70, 9)]
+    a = Case(lens, 4, 2, 64, BF, seed=16, window=window, max_new=max_new)
+    out, lse = a.check()
+    b, lse2 = Case(lens, 4, 2, 64, BF, seed=16, max_new=max_new).run()
+    assert torch.equal(out, b) and torch.equal(lse, lse2)
+
+
 # chunks: whole prompts, ends inside tiles and steps, fewer places than tokens, single tokens among them
 CHUNKS = [(1, 1), (32, 32), (33, 33), (64, 64), (100, 65), (0, 1), (20, 30), (300, 1), (700, 40), (90, 0), (129, 128), (257, 19)]
 
