@@ -59,6 +59,30 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // one instr
 // long request leave the sums alone.
 constexpr float SLACK = 8.0f;
 
+// Where a row's 16-byte pieces are in LDS: piece c at c ^ key_swap(row), c ^ value_swap(row).  A
+// read of 16 bytes a lane takes 16 lanes at a time, 16 keys' piece c here: they have to lie in
+// 16 places of 256 bytes, the banks' width.  A transposed read takes 32 lanes, 64 bytes of four
+// rows that begin at a multiple of four: in four places of 64.
+template <int D>
+__device__ __forceinline__ int key_swap(int row) {
+  return D == 64 ? row >> 1 & 7 : row & 15;
+}
+template <int D>
+__device__ __forceinline__ int value_swap(int row) {
+  return D == 64 ? 4 * (row >> 1 & 1) : 4 * (row & 3);
+}
+
+// The order in which a wavefront's instructions are issued is the order of the source between
+// these: reads of LDS some products ahead, and weights between products, which the matrix
+// cores take 32 cycles each for.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// x, computed again in every step: what follows from it is not kept in registers across them.
+__device__ __forceinline__ int again(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // What a wavefront keeps of its 32 rows; lane (half, col) holds row col's.
 template <int D>
 struct Rows {
@@ -68,27 +92,59 @@ struct Rows {
   int32_t hi, lo;    // the keys [lo, hi) that the row sees
 };
 
+// The values of 16 keys of a step, V^T as the matrix instruction takes it: read in the order in
+// which S^T leaves the keys.
+template <int D>
+struct Values {
+  u32x2 lo[D / 32], hi[D / 32];
+  __device__ __forceinline__ static int offset(int lane) {  // of column tile 0
+    const int half = lane >> 5, j = lane & 15;
+    const int r = 4 * half + j / 4, c = 2 * ((lane >> 4) & 1) + (j % 4) / 2;
+    return r * 2 * D + ((c ^ value_swap<D>(r)) * 16) + (j & 1) * 8;
+  }
+  __device__ __forceinline__ void read(const char *vl, int off, int t, int i) {
+    constexpr int ROWB = 2 * D;
+    const char *x = vl + (off ^ (64 * i));  // (r + 8, r + 16: the same exchange)
+    lo[i] = read_transposed(x + 16 * t * ROWB);
+    hi[i] = read_transposed(x + (16 * t + 8) * ROWB);
+  }
+  __device__ __forceinline__ void read(const char *vl, int off, int t) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) read(vl, off, t, i);
+  }
+};
+
 // One step's 64 keys: the scores.  S^T: lane (half, col) gets row col's scores of keys kb +
 // 32 j + 8 (r / 4) + 4 half + r % 4, -inf for those that the row does not see (MASKED: there
-// may be some).  Returns the row's largest.
+// may be some).  Returns the row's largest, and the first 16 keys' values on their way.
 template <typename T, int D, bool MASKED>
-__device__ __forceinline__ float scores(const Rows<D> &w, const char *kl, int32_t kb, float sc, int lane,
-                                        f32x16 (&s)[2]) {
-  constexpr int STEPS = D / 16, ROWB = 2 * D, KSW = D == 64 ? 7 : 15;
-  const int col = lane & 31, half = lane >> 5;
+__device__ __forceinline__ float scores(const Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc, int lane,
+                                        f32x16 (&s)[2], Values<D> &first) {
+  constexpr int N = D / 8, AHEAD = 6, ROWB = 2 * D;
+  const int l = again(lane), col = l & 31, swap = 16 * ((l >> 5) ^ key_swap<D>(col));
+  const char *row = kl + col * ROWB;
+  const auto piece = [&](int n) {  // (32 rows on: the same exchange)
+    return *reinterpret_cast<const u32x4 *>(row + ((n / 2 * 32) ^ swap) + n % 2 * (32 * ROWB));
+  };
+  u32x4 k[AHEAD];
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n) k[n] = piece(n);
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
 #pragma unroll
-  for (int t = 0; t < STEPS; ++t)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int kr = 32 * j + col;
-      const u32x4 k = *reinterpret_cast<const u32x4 *>(kl + kr * ROWB + (((2 * t + half) ^ (kr & KSW)) * 16));
-      s[j] = T::mfma32(k, w.q[t], s[j]);
-    }
+  for (int n = 0; n < N; ++n) {
+    in_order();
+    if (n == 0) __builtin_amdgcn_s_setprio(1);
+    s[n % 2] = T::mfma32(k[n % AHEAD], w.q[n / 2], s[n % 2]);
+    if (n + AHEAD < N) k[n % AHEAD] = piece(n + AHEAD);
+  }
+  in_order();
+  __builtin_amdgcn_s_setprio(0);
+  first.read(vl, Values<D>::offset(again(lane)), 0);
   if (MASKED) {
+    const int half = lane >> 5;
     const int32_t hi = w.hi - kb - 4 * half, lo = w.lo - kb - 4 * half;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -112,31 +168,40 @@ __device__ __forceinline__ float exponent(const Rows<D> &w) {  // of weight 2^P_
   return T::P_SHIFT - (w.m == -INFINITY ? 0.0f : w.m);
 }
 
-// The weights, 16 keys' at a time, and the products of the 16 before them with their values.
+// The products of 16 keys' weights with their values, among them the next 16's weights and reads.
 template <typename T, int D>
-__device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, int lane,
-                                         const f32x16 (&s)[2]) {
-  constexpr int DT = D / 32, ROWB = 2 * D, VSW = D == 64 ? 3 : 7;
-  const int half = lane >> 5, j = lane & 15;
+__device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, int lane, const f32x16 (&s)[2],
+                                         const Values<D> &first) {
+  constexpr int DT = D / 32;
   const float base = exponent<T>(w);
+  const int off = Values<D>::offset(again(lane));
+  Values<D> v[2];
+  u32x4 p[2];
+  v[0] = first;
+  const auto weights = [&](int t, int e) {
+    const float x = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e], sc, base));
+    const float y = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e + 1], sc, base));
+    w.l += x + y;
+    p[t % 2][e] = T::pack(x, y);
+  };
 #pragma unroll
-  for (int t = 0; t < KT / 16; ++t) {
-    u32x4 p;
+  for (int e = 0; e < 4; ++e) weights(0, e);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e], sc, base));
-      const float y = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e + 1], sc, base));
-      w.l += x + y;
-      p[e] = T::pack(x, y);
-    }
+  for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
     for (int i = 0; i < DT; ++i) {
-      const int r = 16 * t + 4 * half + j / 4, c = 4 * i + 2 * ((lane >> 4) & 1) + (j % 4) / 2;
-      const u32x2 v0 = read_transposed(vl + r * ROWB + ((c ^ (2 * (r & VSW))) * 16) + (j & 1) * 8);
-      const u32x2 v1 = read_transposed(vl + (r + 8) * ROWB + ((c ^ (2 * ((r + 8) & VSW))) * 16) + (j & 1) * 8);
-      w.o[i] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p, w.o[i]);
+      in_order();
+      if (t == 0 && i == 0) __builtin_amdgcn_s_setprio(1);
+      const Values<D> &x = v[t % 2];
+      w.o[i] = T::mfma32(u32x4{x.lo[i].x, x.lo[i].y, x.hi[i].x, x.hi[i].y}, p[t % 2], w.o[i]);
+      if (t + 1 < KT / 16) {
+        v[(t + 1) % 2].read(vl, off, t + 1, i);
+#pragma unroll
+        for (int e = 4 * i / DT; e < 4 * (i + 1) / DT; ++e) weights(t + 1, e);
+      }
     }
-  }
+  in_order();
+  __builtin_amdgcn_s_setprio(0);
 }
 
 // The products where some value is not finite and rows differ in what they see: 0 times it
@@ -144,7 +209,7 @@ __device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, i
 template <typename T, int D>
 __device__ __forceinline__ void products_apart(Rows<D> &w, const char *vl, int32_t kb, float sc, int lane,
                                                f32x16 (&s)[2]) {
-  constexpr int DT = D / 32, ROWB = 2 * D, VSW = D == 64 ? 3 : 7;
+  constexpr int DT = D / 32, ROWB = 2 * D;
   const int col = lane & 31, half = lane >> 5;
   const float base = exponent<T>(w);
   float pair = 0.0f;
@@ -162,7 +227,7 @@ __device__ __forceinline__ void products_apart(Rows<D> &w, const char *vl, int32
       for (int i = 0; i < DT; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {  // components 32 i + 8 g + 4 half + 0 .. 3
-          const u32x2 x2 = *reinterpret_cast<const u32x2 *>(vl + vrow * ROWB + (((4 * i + g) ^ (2 * (vrow & VSW))) * 16) +
+          const u32x2 x2 = *reinterpret_cast<const u32x2 *>(vl + vrow * ROWB + (((4 * i + g) ^ value_swap<D>(vrow)) * 16) +
                                                             half * 8);
           const float v[4] = {T::lo(x2.x), T::hi(x2.x), T::lo(x2.y), T::hi(x2.y)};
 #pragma unroll
@@ -204,7 +269,8 @@ __device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown
 template <typename T, int D, bool ENDS>
 __device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc, bool odd, int lane) {
   f32x16 s[2];
-  const float mx = scores<T, D, ENDS>(w, kl, kb, sc, lane, s);
+  Values<D> first;
+  const float mx = scores<T, D, ENDS>(w, kl, vl, kb, sc, lane, s, first);
   const uint64_t grown = __ballot(mx > w.m + SLACK);  // also the first time: m is -inf
   const float mn = grown ? fmaxf(w.m, mx) : w.m;
   const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
@@ -215,7 +281,45 @@ __device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl,
   if (ENDS && odd)
     products_apart<T>(w, vl, kb, sc, lane, s);
   else
-    products<T>(w, vl, sc, lane, s);
+    products<T>(w, vl, sc, lane, s, first);
+}
+
+// A wavefront's rows: the output, or the sums for the joining.
+template <typename T, int D>
+__device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &it, const Rows<D> &w, int32_t kvh, int wave,
+                                           int lane, float vs) {
+  constexpr int DT = D / 32;
+  const int col = lane & 31, half = lane >> 5;
+  const int32_t row = it.tile * MANY_ROWS + 32 * wave + col, tok = row / a.group, head = kvh * a.group + row % a.group;
+  const bool has_row = row < it.n_new * a.group;
+  if (it.part < 0) {
+    const float inv = w.l == 0.0f ? 0.0f : vs / w.l;
+    uint16_t *p = a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; g += 2) {
+        u32x4 x;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {  // halves trade 4 components: each then has 8 in a row
+          const u32x2 z = swap32(T::pack(w.o[i][4 * g + 2 * e] * inv, w.o[i][4 * g + 2 * e + 1] * inv),
+                                 T::pack(w.o[i][4 * g + 4 + 2 * e] * inv, w.o[i][4 * g + 4 + 2 * e + 1] * inv));
+          x[e] = z.x;
+          x[2 + e] = z.y;
+        }
+        if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
+      }
+    if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of<T>(w.m, w.l);
+  } else if (has_row) {
+    const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + 32 * i + 8 * g + 4 * half) =
+            f32x4{w.o[i][4 * g] * vs, w.o[i][4 * g + 1] * vs, w.o[i][4 * g + 2] * vs, w.o[i][4 * g + 3] * vs};
+    if (half == 0) a.parts.ml[slot] = f32x2{w.m, w.l};
+  }
 }
 
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
@@ -228,7 +332,6 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
   constexpr int NL = KT / RPL;        // loads of a lane per step and side
   constexpr int STEPS = D / 16, DT = D / 32;
   constexpr int ROWB = 2 * D;         // bytes of a row in LDS
-  constexpr int KSW = D == 64 ? 7 : 15, VSW = D == 64 ? 3 : 7;  // exchange of 16-byte pieces within a row
   constexpr int SIDE = KT * ROWB;     // bytes of a step's keys, and of its values
   __shared__ __attribute__((aligned(1024))) char lds[4 * SIDE];  // a step's keys, values; the next one's
   __shared__ int32_t odd_step;  // the last step with a value that is not finite
@@ -321,7 +424,7 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int r = i * RPL + wave * RPW;  // the wavefront's first row
-        const int kc = KV8 ? lcol : lcol ^ ((r + lrow) & KSW), vc = KV8 ? lcol : lcol ^ (2 * ((r + lrow) & VSW));
+        const int kc = KV8 ? lcol : lcol ^ key_swap<D>(r + lrow), vc = KV8 ? lcol : lcol ^ value_swap<D>(r + lrow);
         uint64_t kp, vp;
         uint32_t ko = kc * 16, vo = vc * 16;
         if (WIDE) {
@@ -357,10 +460,10 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
         for (int h = 0; h < 2; ++h) {
           const u32x4 k = kr[i], v = vr[i];
           const uint32_t x = h ? k.z : k.x, y = h ? k.w : k.y, z = h ? v.z : v.x, u = h ? v.w : v.y;
-          *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((2 * lcol + h) ^ (r & KSW)) * 16) =
+          *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((2 * lcol + h) ^ key_swap<D>(r)) * 16) =
               u32x4{T::template from_e4m3<false>(x), T::template from_e4m3<true>(x), T::template from_e4m3<false>(y),
                     T::template from_e4m3<true>(y)};
-          *reinterpret_cast<u32x4 *>(vl + r * ROWB + ((2 * lcol + h) ^ (2 * (r & VSW))) * 16) =
+          *reinterpret_cast<u32x4 *>(vl + r * ROWB + ((2 * lcol + h) ^ value_swap<D>(r)) * 16) =
               u32x4{T::template from_e4m3<false>(z), T::template from_e4m3<true>(z), T::template from_e4m3<false>(u),
                     T::template from_e4m3<true>(u)};
         }
@@ -432,34 +535,7 @@ __global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a
       w.l = __uint_as_float(both.x) + __uint_as_float(both.y);
     }
     const float vs = KV8 && a.cache.v_scale ? a.cache.v_scale[kvh] : 1.0f;
-    if (it.part < 0) {
-      const float inv = w.l == 0.0f ? 0.0f : vs / w.l;
-      uint16_t *p = a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head;
-#pragma unroll
-      for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; g += 2) {
-          u32x4 x;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {  // halves trade 4 components: each then has 8 in a row
-            const u32x2 z = swap32(T::pack(w.o[i][4 * g + 2 * e] * inv, w.o[i][4 * g + 2 * e + 1] * inv),
-                                   T::pack(w.o[i][4 * g + 4 + 2 * e] * inv, w.o[i][4 * g + 4 + 2 * e + 1] * inv));
-            x[e] = z.x;
-            x[2 + e] = z.y;
-          }
-          if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
-        }
-      if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of<T>(w.m, w.l);
-    } else if (has_row) {
-      const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
-#pragma unroll
-      for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + 32 * i + 8 * g + 4 * half) =
-              f32x4{w.o[i][4 * g] * vs, w.o[i][4 * g + 1] * vs, w.o[i][4 * g + 2] * vs, w.o[i][4 * g + 3] * vs};
-      if (half == 0) a.parts.ml[slot] = f32x2{w.m, w.l};
-    }
+    write_rows<T>(a, it, w, kvh, wave, again(lane), vs);
   }
 }
 
