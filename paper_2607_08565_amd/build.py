@@ -1,16 +1,18 @@
-"""Build libsmetric.so for gfx950 with hipcc (always recompiles)."""
+"""Build libsmetric.so for gfx950 with hipcc and the binding of the paged cache's calls (always recompiles)."""
 from __future__ import annotations
 
 import concurrent.futures as cf
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsmetric.so")
+CALLS = os.path.join(HERE, "_kv_calls.so")
 SOURCES = ["hash.hip", "probe.hip", "match.hip", "route.hip", "index.hip", "session.hip", "metrics.hip", "score.hip",
            "kv_rotate.hip", "kv_plan.hip", "kv_few.hip", "kv_many.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -30,9 +32,38 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _compile_calls() -> str:
+    """The Python module behind kv.py: host code against torch's headers."""
+    import torch
+    at = torch.__path__[0]
+    obj = os.path.join(BUILD, "kv_calls.o")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(at, "include"),
+           "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
+           "-c", os.path.join(CSRC, "kv_calls.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for kv_calls.cpp:\n{r.stderr}")
+    return obj
+
+
+def _link_calls(obj: str):
+    import torch
+    tmp = CALLS + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-shared", obj, "-o", tmp, "-L", HERE, "-l:libsmetric.so", "-Wl,-rpath,$ORIGIN",
+           "-L", os.path.join(torch.__path__[0], "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed:\n{r.stderr}")
+    os.replace(tmp, CALLS)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        calls = ex.submit(_compile_calls)
         objs = list(ex.map(_compile, SOURCES))
     tmp = LIB + ".tmp"
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp]
@@ -40,6 +71,7 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, LIB)
+    _link_calls(calls.result())
     if verbose:
         print(f"built {LIB}")
     return LIB

@@ -1,7 +1,7 @@
 """The instance's side of a routed request: the paged KV cache and what writes and reads it.
 
-A thin ctypes binding of include/smetric_kv.h.  A step of a model's layer on a batch of
-requests, each with one new token or a chunk of them:
+A thin binding of include/smetric_kv.h (the calls themselves in csrc/kv_calls.cpp).  A step of a
+model's layer on a batch of requests, each with one new token or a chunk of them:
 
     plan.make(q_off, kv_len)                                    # once per step
     q = kv.append(cache, table, q_off, kv_len, k, v, q=q, rotary=rotary)  # per layer
@@ -12,19 +12,13 @@ Tensors go in by data pointer on torch's current stream; there is no CPU fallbac
 from __future__ import annotations
 
 import ctypes as C
-import struct
 
 import torch
 
-from .smetric import EINVAL, SmetricError, _check, _dev, _lib, _stream
+from .smetric import EINVAL, SmetricError, _check, _dev, _lib
+from . import _kv_calls  # after the library that it calls
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
-
-
-# A single token's calls are bound by this file.  smetric_heads and smetric_batch go as packed
-# bytes: a ctypes structure takes 0.6 us to make, these 0.05 (five of them in an append).
-_pack_heads = struct.Struct("Pqq").pack      # data, token_stride, head_stride
-_pack_batch = struct.Struct("PqiiPPq").pack  # table, table_stride, max_pages, n_req, q_off, kv_len, n_tokens
 
 
 class _Cache(C.Structure):
@@ -38,33 +32,8 @@ class _Rotary(C.Structure):
                 ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float)]
 
 
-def _heads(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str) -> bytes:
-    """An activation [tokens, heads, head_dim]; components contiguous, other strides any."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda:
-        raise TypeError(f"{name}: expected a {dtype} CUDA tensor")
-    st = t.stride()
-    if t.shape != shape or st[2] != 1:
-        raise ValueError(f"{name}: expected shape {tuple(shape)} with contiguous components, got {tuple(t.shape)}, "
-                         f"strides {st}")
-    return _pack_heads(t.data_ptr(), st[0], st[1])
-
-
 def _opt(t: torch.Tensor | None, dtype: torch.dtype, name: str):
     return None if t is None else _dev(t, dtype, name)
-
-
-def _batch(t: torch.Tensor, q_off: torch.Tensor, kv_len: torch.Tensor, n_tokens: int) -> bytes:
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or not t.is_cuda or t.dim() != 2:
-        raise TypeError("page_table: expected an int32 CUDA matrix")
-    rows, width = t.shape
-    stride = t.stride()
-    n_req = kv_len.shape[0]
-    if rows != n_req or (width > 1 and stride[1] != 1):
-        raise ValueError(f"page_table: expected {n_req} rows of contiguous entries, got {tuple(t.shape)}")
-    if q_off.shape[0] != n_req + 1:
-        raise ValueError("q_off: expected one entry more than kv_len")
-    return _pack_batch(t.data_ptr(), max(stride[0], width) if n_req < 2 else stride[0], width, n_req,
-                       _dev(q_off, torch.int64, "q_off"), _dev(kv_len, torch.int32, "kv_len"), n_tokens)
 
 
 class PagedCache:
@@ -116,24 +85,11 @@ class Rotary:
         self.c = _Rotary(w[0], w[1], _opt(table, torch.float32, "table") if rot_dim else None,
                          table.shape[0] if rot_dim else 0, rot_dim, int(interleaved), eps)
         self.ref = C.addressof(self.c)
-        self.fits = None  # the type and head_dim that the weights were found to fit
-
-    def check(self, dtype: torch.dtype, head_dim: int):
-        if self.fits == (dtype, head_dim):
-            return
-        for w, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
-            if w is not None and (w.dtype != dtype or w.numel() != head_dim):
-                raise ValueError(f"{name}: expected {head_dim} values of {dtype}")
-        self.fits = (dtype, head_dim)
 
 
-def _type_of(t: torch.Tensor, name: str) -> int:
-    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.bfloat16, torch.float16) or t.dim() != 3:
+def _new(t: torch.Tensor, name: str) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a bfloat16 or float16 CUDA tensor [tokens, heads, head_dim]")
-    return _DTYPES[t.dtype]
-
-
-def _new(t: torch.Tensor) -> torch.Tensor:
     return torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
@@ -141,18 +97,11 @@ def qk_rotate(q: torch.Tensor, k: torch.Tensor, rotary: Rotary, positions: torch
               q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, status: torch.Tensor | None = None):
     """smetric_qk_rotate: queries and keys [tokens, heads, head_dim] normed and rotated to
     their positions (int32).  Outputs may be the inputs.  Returns (q_out, k_out)."""
-    code, dtype, shape = _type_of(q, "q"), q.dtype, q.shape
-    T, Hq, D = shape
-    rotary.check(dtype, D)
-    q_out = _new(q) if q_out is None else q_out
-    k_out = _new(k) if k_out is None else k_out
-    if positions is not None and positions.shape[0] != T:
-        raise ValueError("positions: expected one per token")
-    k_shape = (T, k.shape[1], D)
-    _check("smetric_qk_rotate", _lib.smetric_qk_rotate(
-        code, D, T, rotary.ref, _opt(positions, torch.int32, "positions"), Hq, _heads(q, dtype, shape, "q"),
-        _heads(q_out, dtype, shape, "q_out"), k_shape[1], _heads(k, dtype, k_shape, "k"),
-        _heads(k_out, dtype, k_shape, "k_out"), _opt(status, torch.int32, "status"), _stream()))
+    q_out = _new(q, "q") if q_out is None else q_out
+    k_out = _new(k, "k") if k_out is None else k_out
+    rc = _kv_calls.qk_rotate(q, k, rotary.ref, rotary.q_weight, rotary.k_weight, positions, q_out, k_out, status)
+    if rc:
+        raise SmetricError("smetric_qk_rotate", rc)
     return q_out, k_out
 
 
@@ -162,24 +111,12 @@ def append(cache: PagedCache, page_table: torch.Tensor, q_off: torch.Tensor, kv_
     """smetric_kv_append: the new tokens' keys (normed and rotated) and values into the pages;
     kv_len counts the new tokens already.  With q its queries normed and rotated are
     returned (q_out, may be q)."""
-    code, dtype = _type_of(k, "k"), k.dtype
-    T, D = k.shape[0], cache.head_dim
-    shape = (T, cache.n_kv_heads, D)
-    ref = None
-    if rotary is not None:
-        rotary.check(dtype, D)
-        ref = rotary.ref
-    if positions is not None and positions.shape[0] != T:
-        raise ValueError("positions: expected one per token")
-    Hq, q_in, q_to = 0, None, None
-    if q is not None:
-        q_out = _new(q) if q_out is None else q_out
-        Hq = q.shape[1]
-        q_shape = (T, Hq, D)
-        q_in, q_to = _heads(q, dtype, q_shape, "q"), _heads(q_out, dtype, q_shape, "q_out")
-    _check("smetric_kv_append", _lib.smetric_kv_append(
-        code, cache.ref, _batch(page_table, q_off, kv_len, T), ref, _opt(positions, torch.int32, "positions"), Hq, q_in,
-        q_to, _heads(k, dtype, shape, "k"), _heads(v, dtype, shape, "v"), _opt(status, torch.int32, "status"), _stream()))
+    if q is not None and q_out is None:
+        q_out = _new(q, "q")
+    r = (0, None, None) if rotary is None else (rotary.ref, rotary.q_weight, rotary.k_weight)
+    rc = _kv_calls.append(cache.ref, page_table, q_off, kv_len, k, v, q, q_out, *r, positions, status)
+    if rc:
+        raise SmetricError("smetric_kv_append", rc)
     return q_out if q is not None else None
 
 
@@ -204,13 +141,10 @@ class Plan:
 
     def make(self, q_off: torch.Tensor, kv_len: torch.Tensor, status: torch.Tensor | None = None) -> "Plan":
         """smetric_attend_plan for these lengths (device tensors, read on the current stream)."""
-        n_req, n_tokens = self.args[:2]
-        if kv_len.numel() != n_req or q_off.numel() != n_req + 1:
-            raise ValueError(f"expected {n_req} requests")
+        rc = _kv_calls.make_plan(q_off, kv_len, *self.args, self.window, self.plan_ptr, self.plan_bytes, status)
+        if rc:
+            raise SmetricError("smetric_attend_plan", rc)
         self.q_off, self.kv_len = q_off, kv_len
-        _check("smetric_attend_plan", _lib.smetric_attend_plan(
-            _dev(q_off, torch.int64, "q_off"), _dev(kv_len, torch.int32, "kv_len"), *self.args, self.window,
-            self.plan_ptr, self.plan_bytes, _opt(status, torch.int32, "status"), _stream()))
         return self
 
 
@@ -219,19 +153,15 @@ def attend(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, plan: P
     """smetric_attend: the new tokens' attention over the pages, as `plan` (made for the batch)
     splits it.  scale: 1 / sqrt(head_dim) by default; lse (float32 [tokens, heads]) is
     filled if given.  Returns out [tokens, heads, head_dim]."""
-    code, dtype = _type_of(q, "q"), q.dtype
     if plan.kv_len is None:
         raise ValueError("plan: make() it for the batch first")
     _, T, Hq, H, D, max_new = plan.args
     if H != cache.n_kv_heads or D != cache.head_dim:
         raise ValueError("plan and cache differ in heads or head_dim")
-    out = _new(q) if out is None else out
-    if lse is not None and lse.shape != (T, Hq):
-        raise ValueError(f"lse: expected shape {(T, Hq)}")
-    shape = (T, Hq, D)
-    _check("smetric_attend", _lib.smetric_attend(
-        code, cache.ref, _batch(page_table, plan.q_off, plan.kv_len, T), Hq, _heads(q, dtype, shape, "q"),
-        _heads(out, dtype, shape, "out"), _opt(lse, torch.float32, "lse"), D ** -0.5 if scale is None else scale, max_new,
-        plan.window, plan.plan_ptr, plan.plan_bytes, plan.ws_ptr, plan.ws_bytes, _opt(status, torch.int32, "status"),
-        _stream()))
+    out = _new(q, "q") if out is None else out
+    rc = _kv_calls.attend(q, out, lse, cache.ref, page_table, plan.q_off, plan.kv_len, T, Hq,
+                          D ** -0.5 if scale is None else scale, max_new, plan.window, plan.plan_ptr, plan.plan_bytes,
+                          plan.ws_ptr, plan.ws_bytes, status)
+    if rc:
+        raise SmetricError("smetric_attend", rc)
     return out

@@ -87,7 +87,7 @@ def _load() -> C.CDLL:
         "smetric_match_probed": [PIX, P, U64, P, P, I32, I64, P, P],
         "smetric_index_insert_probed": [PIX, P, U64, I32, I64, P, P, U32, P, U64, P],
         "smetric_route_score": [I32, P, I32, I32, P, P, P, I32, I32, I32, U64, P, P, P],
-        # the instance's side (smetric_kv.h; marshalled by kv.py)
+        # the instance's side (smetric_kv.h; called through kv.py)
         "smetric_qk_rotate": [I32, I32, I64, P, P, I32, P, P, I32, P, P, P, P],
         "smetric_kv_append": [I32, P, P, P, P, I32, P, P, P, P, P, P],
         "smetric_attend_plan_bytes": [I32, I64, I32, I32, I32, I32, P, P],

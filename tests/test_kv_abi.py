@@ -1,5 +1,6 @@
 """The paged cache's entry points on the host: sizes and refusals (no GPU work is launched)."""
 import ctypes as C
+import struct
 
 import pytest
 
@@ -9,7 +10,7 @@ FAKE = 1 << 20  # an aligned address that nothing reads: every call below return
 
 
 def heads(data=FAKE, token=256, head=64):
-    return kv._pack_heads(data, token, head)
+    return struct.pack("Pqq", data, token, head)
 
 
 def cache(**how):
@@ -27,7 +28,7 @@ def rotary(**how):
 
 
 def batch(table=FAKE, stride=4, pages=4, n_req=2, q_off=FAKE, kv_len=FAKE, n_tokens=3):
-    return kv._pack_batch(table, stride, pages, n_req, q_off, kv_len, n_tokens)
+    return struct.pack("PqiiPPq", table, stride, pages, n_req, q_off, kv_len, n_tokens)
 
 
 def test_plan_sizes():
