@@ -30,20 +30,23 @@ struct PlanSplit {  // a tile of more than one piece
 };
 struct PlanHdr {
   int32_t err, n_items, n_splits, n_groups;
-  int32_t n_req, n_q, n_kv, rows, window, pad0;
+  int32_t n_req, n_q, n_kv, rows, window, dim;
   int64_t n_tokens;
   int32_t pad[20];
 };
 static_assert(sizeof(PlanHdr) == 128 && sizeof(PlanItem) == 32 && sizeof(PlanSplit) == 32, "plan layout");
 
-// Workgroups of a step, over all key-value heads: as many as run at once (two on each of 256
-// compute units), each with an equal share of the key steps in order, so that all end
-// together; a share begins and ends within a tile, which is then in pieces, and may hold
-// several tiles.  Two exceptions: no share is smaller than MIN_STEPS, and a cut this near a
-// tile's end goes to the end (EDGE_STEPS).  Few rows: a step is half a block of each
-// wavefront, so two make the shortest share that occupies all four (one token over 1,025 keys:
-// 5.8 us, with shares of four steps 8.3, of eight 11.6).
-constexpr int32_t TARGET = 512;
+// Workgroups of a step, over all key-value heads: as many as run at once (on each of 256
+// compute units two, one with heads of 256: their registers), each with an equal share of the
+// key steps in order, so that all end together; a share begins and ends within a tile, which is
+// then in pieces, and may hold several tiles.  Heads of 64 would leave room for three, which is
+// no faster (4 chunks of 2,048 over 8-bit pages: 740 us, with two 702); heads of 256 with twice
+// as many shares as run at once: 2 chunks of 2,048 910 us for 858, 65,536 keys 59 for 53.
+// Two exceptions: no share is smaller than MIN_STEPS, and a cut this near a tile's end goes to
+// the end (EDGE_STEPS).  Few rows: a step is half a block of each wavefront, so two make the
+// shortest share that occupies all four (one token over 1,025 keys: 5.8 us, with shares of four
+// steps 8.3, of eight 11.6).
+constexpr int32_t at_once(int32_t head_dim) { return head_dim == 256 ? 1 : 2; }
 constexpr int32_t FEW_MIN_STEPS = 2, FEW_EDGE_STEPS = 1, FEW_TILE_COST = 0;
 constexpr int32_t MANY_MIN_STEPS = 8, MANY_EDGE_STEPS = 4, MANY_TILE_COST = 2;
 
@@ -60,7 +63,7 @@ struct PlanShape {
 inline PlanShape plan_shape(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t max_new) {
   PlanShape s;
   s.rows = rows_per_tile(n_q, n_kv, max_new);
-  s.target = TARGET / n_kv;
+  s.target = 256 * at_once(head_dim) / n_kv;
   if (s.target < 1) s.target = 1;
   s.max_tiles = n_tokens * (n_q / n_kv) / s.rows + n_req;
   s.max_items = s.max_tiles + s.target;
@@ -91,13 +94,13 @@ struct AttendArgs {
   PartView parts;
   int64_t n_tokens;
   int32_t n_req, n_q, n_kv, group;  // group = n_q / n_kv
-  int32_t rows, window;
+  int32_t rows, dim, window;
   float scale_log2;  // scale * log2(e)
   int32_t *status;
 };
 __device__ __forceinline__ bool plan_fits(const AttendArgs &a, const PlanHdr &h) {
   return h.err == 0 && h.n_req == a.n_req && h.n_q == a.n_q && h.n_kv == a.n_kv && h.rows == a.rows &&
-         h.window == a.window && h.n_tokens == a.n_tokens;
+         h.dim == a.dim && h.window == a.window && h.n_tokens == a.n_tokens;
 }
 
 // lse from a row's maximum (in powers of two) and sum of weights.

@@ -44,7 +44,7 @@ __device__ __forceinline__ float sum4(float x) {
 
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
 template <typename T, bool KV8, int D, bool WIDE>
-__global__ __launch_bounds__(64 * FW, D == 256 ? 1 : 2) void few_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) {
   constexpr int ESZ = KV8 ? 1 : 2;
   constexpr int STEPS = D / 32;               // matrix steps over the components
   constexpr int KL = D * ESZ / 64;            // 16-byte loads of a lane for 16 keys

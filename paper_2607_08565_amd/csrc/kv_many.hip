@@ -324,7 +324,7 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
 
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
 template <typename T, bool KV8, int D, bool WIDE>
-__global__ __launch_bounds__(MT, D == 256 ? 1 : 2) void many_kernel(AttendArgs a) {
+__global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
   constexpr int ESZ = KV8 ? 1 : 2;
   constexpr int LPR = D * ESZ / 16;   // lanes per row of keys or values
   constexpr int RPW = 64 / LPR;       // rows of a wavefront's load

@@ -18,7 +18,7 @@ constexpr int32_t CUT_COST = 12;   // steps: what a share's partial results cost
 struct PlanArgs {
   const int64_t *q_off;
   const int32_t *kv_len;
-  int32_t n_req, n_q, n_kv, group, rows, rows_log2, window, target, min_steps, edge_steps, tile_cost;
+  int32_t n_req, n_q, n_kv, group, dim, rows, rows_log2, window, target, min_steps, edge_steps, tile_cost;
   int64_t n_tokens, max_tiles, max_items, max_groups, max_splits, max_parts;
   PlanHdr *hdr;
   PlanItem *items;
@@ -214,6 +214,7 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
     h.n_q = a.n_q;
     h.n_kv = a.n_kv;
     h.rows = a.rows;
+    h.dim = a.dim;
     h.window = a.window;
     h.n_tokens = a.n_tokens;
     *a.hdr = h;
@@ -341,7 +342,7 @@ extern "C" int smetric_attend_plan(const int64_t *q_off, const int32_t *kv_len, 
   const PlanShape s = plan_shape(n_req, n_tokens, n_q_heads, n_kv_heads, head_dim, max_new);
   if (plan_bytes < s.plan_bytes) return SMETRIC_EWORKSPACE;
   char *p = static_cast<char *>(plan);
-  PlanArgs a{q_off, kv_len, n_req, n_q_heads, n_kv_heads, n_q_heads / n_kv_heads, s.rows, s.rows == FEW_ROWS ? 4 : 7, window_of(window), s.target,
+  PlanArgs a{q_off, kv_len, n_req, n_q_heads, n_kv_heads, n_q_heads / n_kv_heads, head_dim, s.rows, s.rows == FEW_ROWS ? 4 : 7, window_of(window), s.target,
              s.rows == FEW_ROWS ? FEW_MIN_STEPS : MANY_MIN_STEPS, s.rows == FEW_ROWS ? FEW_EDGE_STEPS : MANY_EDGE_STEPS,
              s.rows == FEW_ROWS ? FEW_TILE_COST : MANY_TILE_COST,
              n_tokens, n_req ? s.max_tiles : 0, s.max_items, s.max_groups, s.max_splits, s.max_parts,
@@ -385,6 +386,7 @@ extern "C" int smetric_attend(int32_t dtype, const smetric_kv_cache *cache, cons
   a.n_kv = cache->n_kv_heads;
   a.group = n_q_heads / cache->n_kv_heads;
   a.rows = s.rows;
+  a.dim = cache->head_dim;
   a.window = window_of(window);
   a.scale_log2 = scale * 1.4426950408889634f;
   a.status = status;
