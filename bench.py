@@ -443,11 +443,13 @@ def summarize_sq(csv_path: str, steps: int, bench_json: str):
 
 
 def kernel_sources_hash() -> str:
+    """Of the sources that the benchmark's kernels are built from (kv_*: the paged cache's)."""
     import glob
     import hashlib
     h = hashlib.sha256()
     for f in sorted(glob.glob(os.path.join(ROOT, "paper_2607_08565_amd", "csrc", "*"))):
-        h.update(open(f, "rb").read())
+        if not os.path.basename(f).startswith("kv_"):
+            h.update(open(f, "rb").read())
     return h.hexdigest()[:16]
 
 
