@@ -144,6 +144,16 @@ def test_long_requests_are_split(lens, fp8):
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("R,most", [(600, 1), (2100, 1), (600, 9), (2100, 5)])
+@pytest.mark.parametrize("window", [0, 7])
+def test_many_requests(R, most, window):
+    """More requests and tiles than one pass of the plan holds, some without tokens, some longer than the rest."""
+    lens = [((i * 37) % 61 + (900 if i % 97 == 5 else 0), 0 if i % 13 == 4 else i % most + 1) for i in range(R)]
+    Case(lens, 2, 1, 64, BF, seed=17, window=window).check()
+    if most > 1:
+        Case(lens, 2, 1, 64, BF, seed=17, window=window, max_new=1000).check()
+
+
 def test_large_scores():
     """Scores of hundreds, maxima that keep growing along the keys and ones that come first."""
     for sign in (1, -1):
