@@ -128,7 +128,7 @@ struct Values {
 template <typename T, int D, bool MASKED>
 __device__ __forceinline__ float scores(const Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc, int lane,
                                         f32x16 (&s)[2], Values<D> &first) {
-  constexpr int N = D / 8, AHEAD = 6, ROWB = 2 * D;
+  constexpr int N = D / 8, AHEAD = 4, ROWB = 2 * D;
   const int l = again(lane), col = l & 31, swap = 16 * ((l >> 5) ^ key_swap<D>(col));
   const char *row = kl + col * ROWB;
   const auto piece = [&](int n) {  // (32 rows on: the same exchange)
@@ -280,10 +280,13 @@ __device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl,
   Values<D> first;
   const float mx = scores<T, D, ENDS>(w, kl, vl, kb, sc, lane, s, first);
   const uint64_t grown = __ballot(mx > w.m + SLACK);  // also the first time: m is -inf
-  const float mn = grown ? fmaxf(w.m, mx) : w.m;
-  const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
-  w.m = mn;
-  w.l *= down;
+  float down = 1.0f;
+  if (grown) {
+    const float mn = fmaxf(w.m, mx);
+    down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
+    w.m = mn;
+    w.l *= down;
+  }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
   if (ENDS && odd)
