@@ -74,21 +74,20 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t d) {
 }
 
 // Sum of x over the workgroup's earlier threads; total: over all.
-template <typename N>
-__device__ N scan(N x, N &total, N *sh) {
+__device__ int64_t scan(int64_t x, int64_t &total, int64_t *sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  N a = x;
+  int64_t a = x;
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) {
-    const N u = __shfl_up(a, m, 64);
+    const int64_t u = __shfl_up(a, m, 64);
     if (lane >= m) a += u;
   }
   if (lane == 63) sh[wave] = a;
   __syncthreads();
-  N before = 0;
+  int64_t before = 0;
   total = 0;
   for (int w = 0; w < PT / 64; ++w) {
-    const N v = sh[w];
+    const int64_t v = sh[w];
     before += w < wave ? v : 0;
     total += v;
   }
@@ -111,7 +110,6 @@ __device__ bool whole_tiles(int64_t cost, int64_t tiles, int32_t longest, int32_
 __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
   static_assert(FEW_ROWS == 1 << 4 && MANY_ROWS == 1 << 7, "rows_log2");
   __shared__ int64_t sh64[PT / 64];
-  __shared__ int32_t sh32[PT / 64];
   __shared__ int64_t off_l[STAGED + 1];
   __shared__ int32_t len_l[STAGED];
   __shared__ int bad, longest;
@@ -149,8 +147,11 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
     }
     atomicMax(&longest, top);
     int64_t cost, tiles;
-    scan<int64_t>(mine, cost, sh64);
-    scan<int64_t>(count, tiles, sh64);
+    const int64_t before = scan(mine, cost, sh64);
+    if (a.max_tiles <= PT)
+      tiles = __syncthreads_count(count);
+    else
+      scan(count, tiles, sh64);
     const int32_t least = a.min_steps + a.tile_cost;
     int64_t groups = quotient(cost + least - 1, least);
     if (groups > a.target) groups = a.target;
@@ -165,9 +166,12 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
       if (a.max_tiles > PT || g >= a.max_tiles) t.req = -1;
       if (a.max_tiles > PT && g < a.max_tiles) t = tile_at(a, q_off, kv_len, g);
       const int64_t c = t.req < 0 ? 0 : cost_of(a, t);
-      int64_t all;
-      const int64_t at = at0 + scan<int64_t>(c, all, sh64);
-      at0 += all;
+      int64_t at = before;
+      if (a.max_tiles > PT) {
+        int64_t all;
+        at = at0 + scan(c, all, sh64);
+        at0 += all;
+      }
       // shares' ends at multiples of `share`: w_lo .. w_hi cut this tile
       int64_t w_lo = 0, w_hi = -1;
       if (t.req >= 0 && !whole) {
@@ -176,10 +180,10 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
         if (w_hi >= n_groups) w_hi = n_groups - 1;
       }
       const int32_t cuts = w_hi >= w_lo ? int32_t(w_hi - w_lo + 1) : 0, pieces = t.req < 0 ? 0 : cuts + 1;
-      int32_t all_p, all_c, all_s;
-      const int64_t base = n_items + scan<int32_t>(pieces, all_p, sh32);
-      const int64_t part0 = n_parts + scan<int32_t>(cuts ? pieces : 0, all_c, sh32);
-      const int64_t split_at = n_splits + scan<int32_t>(cuts > 0, all_s, sh32);
+      // in one scan: pieces, those of cut tiles (at most 2 target, 16 bits), cut tiles (16 bits)
+      int64_t all_n;
+      const int64_t n = scan(int64_t(pieces) << 32 | int64_t(cuts ? pieces : 0) << 16 | (cuts > 0), all_n, sh64);
+      const int64_t base = n_items + (n >> 32), part0 = n_parts + (n >> 16 & 0xFFFF), split_at = n_splits + (n & 0xFFFF);
       const int32_t k = t.k0 / KEY_STEP;
       for (int32_t i = 0; i < pieces && base + i < a.max_items; ++i) {
         const int32_t c0 = i ? int32_t((w_lo + i - 1) * share - at) - a.tile_cost : 0;
@@ -195,9 +199,9 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
         for (int64_t w = quotient(at + share - 1, share); w * share < at + c && w < n_groups && w < a.max_groups; ++w)
           a.first[w] = int32_t(base + (w < w_lo ? 0 : w > w_hi ? pieces : w - w_lo + 1));
       }
-      n_items += all_p;
-      n_parts += all_c;
-      n_splits += all_s;
+      n_items += all_n >> 32;
+      n_parts += all_n >> 16 & 0xFFFF;
+      n_splits += all_n & 0xFFFF;
     }
   }
   if (threadIdx.x == 0) {

@@ -124,9 +124,17 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
   int64_t page_row = 0;
   bool ok = live, bad = false;
   if (PAGED) {
-    const int32_t r = request_of(ba.q_off, ba.n_req, t0 < n_tokens ? t0 : n_tokens - 1, t, lane);
-    const int64_t a = ba.q_off[r], z = ba.q_off[r + 1];
-    const int32_t len = ba.kv_len[r];
+    // In a decoding step token t is request t's: asked for at once; a search of the whole
+    // wavefront where that is not so for one of its lanes.
+    int32_t r = t < ba.n_req ? int32_t(t) : ba.n_req - 1;
+    int64_t a = ba.q_off[r], z = ba.q_off[r + 1];
+    int32_t len = ba.kv_len[r];
+    if (__any(a > t || z <= t)) {
+      r = request_of(ba.q_off, ba.n_req, t0 < n_tokens ? t0 : n_tokens - 1, t, lane);
+      a = ba.q_off[r];
+      z = ba.q_off[r + 1];
+      len = ba.kv_len[r];
+    }
     bad = t < a || t >= z || len < 0 || len > MAX_PLACES || int64_t(len) > int64_t(cache.max_pages) * cache.ps.size;
     const int64_t p = int64_t(len) - (z - t);
     ok = ok && !bad && p >= 0;
