@@ -15,8 +15,8 @@
 // leaves them is used.  The next 32 keys' loads are in flight during all of it.
 //
 // Measured: 32 requests decoding over 1.73 GB of cache 303 us, 5.7 TB/s (a copy of 4 GiB moves
-// 4.8); 64 drafted tokens over 0.58 GB 115 us; 131,072 keys of 8 bits (134 MB) 31 to 34 us, 24
-// of them here and the rest the joining; a lone token over 1,025 keys 9.2 us, two launches.
+// 4.8); 64 drafted tokens over 0.58 GB 115 us; 131,072 keys of 8 bits (134 MB) 31 to 35 us, 24
+// of them here and the rest the joining; a lone token over 1,025 keys 9.5 us, two launches.
 #include <math.h>
 
 #include "kv_attend.h"

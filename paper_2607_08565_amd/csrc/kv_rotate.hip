@@ -13,8 +13,8 @@
 // cosines and sines come from memory once and from the nearest cache for its other heads.
 //
 // Measured: 8,191 tokens of 40 heads of 128 32.1 us, 5.3 TB/s (a copy of 4 GiB moves 4.8); the
-// keys, values and queries of 6,249 tokens appended 37.8 us, 4.2 TB/s (pages in any order, the
-// queries kept in the caches for the attention); a token's append 4.5 us, its launch.
+// keys, values and queries of 6,249 tokens appended 38.1 us, 4.1 TB/s (pages in any order, the
+// queries kept in the caches for the attention); a token's append 4.4 us, its launch; of 256 5.3.
 #include "common.h"
 #include "kv_common.h"
 
