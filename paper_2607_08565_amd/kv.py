@@ -16,7 +16,11 @@ import ctypes as C
 import torch
 
 from .smetric import EINVAL, SmetricError, _check, _dev, _lib
-from . import _kv_calls  # after the library that it calls
+
+try:
+    from . import _kv_calls
+except ImportError as e:
+    raise RuntimeError("_kv_calls.so is missing or does not fit: build it first (__graft_entry__.build())") from e
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
 
