@@ -45,10 +45,12 @@ static_assert(sizeof(PlanHdr) == 128 && sizeof(PlanItem) == 32 && sizeof(PlanSpl
 // Two exceptions: no share is smaller than MIN_STEPS, and a cut this near a tile's end goes to
 // the end (EDGE_STEPS).  Few rows: a step is half a block of each wavefront, so two make the
 // shortest share that occupies all four (one token over 1,025 keys: 5.8 us, with shares of four
-// steps 8.3, of eight 11.6).
+// steps 8.3, of eight 11.6).  Many rows: a short chunk is a chain of steps of one workgroup, so
+// two again (32 tokens over 1,032 keys: 17 us, with shares of eight steps 22; 64 over 4,064 at heads
+// of 128 23 and 30; 30 over 2,030 at heads of 256 28 and 41; long chunks the same).
 constexpr int32_t at_once(int32_t head_dim) { return head_dim == 256 ? 1 : 2; }
 constexpr int32_t FEW_MIN_STEPS = 2, FEW_EDGE_STEPS = 1, FEW_TILE_COST = 0;
-constexpr int32_t MANY_MIN_STEPS = 8, MANY_EDGE_STEPS = 4, MANY_TILE_COST = 2;
+constexpr int32_t MANY_MIN_STEPS = 2, MANY_EDGE_STEPS = 1, MANY_TILE_COST = 2;
 
 struct PlanShape {
   int32_t rows, target;  // rows per tile; workgroups aimed at per key-value head

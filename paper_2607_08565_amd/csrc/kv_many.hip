@@ -13,7 +13,7 @@
 // maximum takes one lane exchange, and its weights are where the second product wants them --
 // the order in which S^T leaves the keys is the order in which V^T is read, transposed, from LDS.
 //
-// Measured: 4,096 tokens over 16,384 (32 heads of 128) 941 us, 1,020 TFLOP/s; the library's product
+// Measured: 4,096 tokens over 16,384 (32 heads of 128) 941 to 990 us from card to card, 1,020 TFLOP/s; the library's product
 // of matrices of 16,384 reaches 1,340, of 8,192 1,130.  The matrix cores work half of the cycles
 // and the vector instructions about as long (33 exponentials, 32 sums, 31 products and 16
 // maxima a step of 32 matrix instructions), on two wavefronts that overlap them in part, at a
