@@ -51,7 +51,7 @@ typedef struct smetric_kv_cache {
   int32_t n_kv_heads;
   int32_t head_dim;                  /* 64, 128 or 256 */
   int32_t dtype;
-  const float *k_scale, *v_scale;    /* float32[n_kv_heads], E4M3: a stored x stands for x * scale */
+  const float *k_scale, *v_scale;    /* float32[n_kv_heads], E4M3: a stored x stands for x * scale, any number */
 } smetric_kv_cache;
 
 /* A ragged batch: request r's new tokens are q_off[r] .. q_off[r+1] of the activations and

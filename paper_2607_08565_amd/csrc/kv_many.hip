@@ -383,12 +383,26 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     if (tile_end > it.n_new * a.group) tile_end = it.n_new * a.group;
     const int32_t tile_max_lo = a.window > 0 ? first + (tile_end - 1) / a.group + 1 - a.window : 0;
 
+    // Scores are masked, and their largest found, before they are multiplied, so the factor has to
+    // be positive: another one's sign goes into the queries, and a NaN; zero becomes the smallest
+    // normal number, which leaves all weights 1 for scores below 2^100.
+    float sc = a.scale_log2;
+    uint32_t flip = 0, nan = 0;
+    if (KV8 && a.cache.k_scale) {
+      sc *= a.cache.k_scale[kvh];
+      if (!(sc > 0.0f)) {
+        flip = sc < 0.0f ? 0x80008000u : 0;
+        nan = sc != sc ? 0x7FFF7FFFu : 0;
+        sc = sc < 0.0f ? -sc : sc == 0.0f ? 0x1p-126f : 1.0f;
+      }
+    }
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       w.q[s] = u32x4{0, 0, 0, 0};
       if (has_row)
         w.q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + s * 16 +
                                                   half * 8);
+      if (KV8) w.q[s] = (w.q[s] ^ flip) | nan;
     }
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -399,7 +413,6 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     const char *kbase = a.cache.k.base + kvh * a.cache.k.head;
     const char *vbase = a.cache.v.base + kvh * a.cache.v.head;
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
-    const float sc = a.scale_log2 * (KV8 && a.cache.k_scale ? a.cache.k_scale[kvh] : 1.0f);
 
     const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
     u32x4 kr[KV8 ? NL : 1], vr[KV8 ? NL : 1];  // 8-bit keys and values on their way to LDS
