@@ -281,10 +281,10 @@ __device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl,
   const float mx = scores<T, D, ENDS>(w, kl, vl, kb, sc, lane, s, first);
   const uint64_t grown = __ballot(mx > w.m + SLACK);  // also the first time: m is -inf
   float down = 1.0f;
-  if (grown) {
-    const float mn = fmaxf(w.m, mx);
-    down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
-    w.m = mn;
+  if (grown) {  // only the rows that have grown: another one's scores change nothing in a row
+    const bool mine = mx > w.m + SLACK;
+    down = mine ? __builtin_amdgcn_exp2f(w.m - mx) : 1.0f;
+    w.m = mine ? mx : w.m;
     w.l *= down;
   }
 #pragma unroll
