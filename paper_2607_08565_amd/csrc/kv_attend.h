@@ -126,6 +126,27 @@ __device__ __forceinline__ bool any_not_finite(u32x4 x) {
   return (c & 0x80008000u) != 0;
 }
 
+// Eight 16-bit floats, zeros for those that are not finite.
+template <typename T>
+__device__ __forceinline__ u32x4 finite_only(u32x4 x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] &= ~((((x[i] & T::EXP) + T::ONE_EXP) >> 15 & 0x00010001u) * 0xFFFFu);
+  return x;
+}
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+// Components c .. c + 3 of a row of values in memory.
+template <typename T, bool KV8>
+__device__ __forceinline__ f32x4 four_values(uint64_t row, int c) {
+  u32x2 x;
+  if (KV8) {
+    const uint32_t y = *reinterpret_cast<const uint32_t *>(row + c);
+    x = u32x2{T::template from_e4m3<false>(y), T::template from_e4m3<true>(y)};
+  } else {
+    x = *reinterpret_cast<const u32x2 *>(row + 2 * c);
+  }
+  return f32x4{T::lo(x.x), T::hi(x.x), T::lo(x.y), T::hi(x.y)};
+}
+
 // 16 lanes read four rows' 16 columns of 16-bit values from LDS, each lane's address a row's
 // (lane / 4) four columns (lane % 4): lane i gets column i of the four rows.
 typedef __attribute__((ext_vector_type(4))) short s16x4;

@@ -175,6 +175,7 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0.0f;
+    bool odd = false;  // a value that rows see differently is not finite
     if (kb0 < k1) {
       if (WIDE) find_blocks(kb0);
       load_block(kb0);
@@ -200,8 +201,16 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
         }
       }
       const bool partial = kb < k0 || kb + FK > k1, masked = kb < max_lo || kb + FK > min_hi;
-      // values to LDS, as 16-bit rows whose 16-byte pieces are exchanged within the row
-      bool odd = false;
+      // values to LDS, as 16-bit rows whose 16-byte pieces are exchanged within the row; zeros in
+      // place of those that are not finite where rows differ in what they see, as 0 times them must
+      // not reach a row that does not see them (added in the end, from memory again, to the rows that
+      // do: weights are positive, infinities and NaN come through as they are)
+      const bool apart = masked && !one_token;
+      const auto finite = [&](u32x4 x) {
+        if (!apart || !any_not_finite<T>(x)) return x;
+        odd = true;
+        return finite_only<T>(x);
+      };
       wave_fence();
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
@@ -213,12 +222,10 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
                         T::template from_e4m3<false>(v.y), T::template from_e4m3<true>(v.y)};
           const u32x4 y{T::template from_e4m3<false>(v.z), T::template from_e4m3<true>(v.z),
                         T::template from_e4m3<false>(v.w), T::template from_e4m3<true>(v.w)};
-          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((2 * c) ^ (2 * (r & SWZ))) * 16)) = x;
-          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((2 * c + 1) ^ (2 * (r & SWZ))) * 16)) = y;
-          if (masked) odd |= any_not_finite<T>(x) || any_not_finite<T>(y);
+          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((2 * c) ^ (2 * (r & SWZ))) * 16)) = finite(x);
+          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((2 * c + 1) ^ (2 * (r & SWZ))) * 16)) = finite(y);
         } else {
-          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + ((c ^ (2 * (r & SWZ))) * 16)) = v;
-          if (masked) odd |= any_not_finite<T>(v);
+          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + ((c ^ (2 * (r & SWZ))) * 16)) = finite(v);
         }
       }
       wave_fence();
@@ -256,36 +263,30 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
         p[e] = __builtin_amdgcn_exp2f(p[e] - base);
         l += p[e];
       }
-      if (masked && !one_token && __any(odd)) {
-        // some value is not finite and rows differ in what they see: 0 times it must not reach
-        // a row that does not see it.  Rare, so plain sums: weight e of lane group g for each.
-#pragma unroll 1
-        for (int e = 0; e < 8; ++e) {
-#pragma unroll 1
-          for (int g = 0; g < 4; ++g) {
-            const float w = __shfl(p[0], col + 16 * g);
-            const int r = 16 * (e / 4) + 4 * g + e % 4, key = kb + r;
-            const bool seen = key < hi && key >= lo;
+      const u32x4 pw{T::pack(p[0], p[1]), T::pack(p[2], p[3]), T::pack(p[4], p[5]), T::pack(p[6], p[7])};
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-              const int c = 2 * i + grp / 2;
-              const u32x2 x = *reinterpret_cast<const u32x2 *>(my + r * (2 * D) + ((c ^ (2 * (r & SWZ))) * 16) + (grp & 1) * 8);
-              const float v[4] = {T::lo(x.x), T::hi(x.x), T::lo(x.y), T::hi(x.y)};
+      for (int i = 0; i < DT; ++i) {
+        const int r = 4 * grp + col / 4, c = 2 * i + (col % 4) / 2;
+        const char *x = my + r * (2 * D) + ((c ^ (2 * (r & SWZ))) * 16) + (col & 1) * 8;
+        const u32x2 v0 = read_transposed(x), v1 = read_transposed(x + 16 * (2 * D));  // r + 16: the same exchange
+        o[i] = T::mfma16(u32x4{v0.x, v0.y, v1.x, v1.y}, pw, o[i]);
+      }
+    }
+    if (!one_token && __any(odd)) {
+#pragma unroll 1
+      for (int32_t kb = kb0; kb < k1; kb += FK * FW) {
+        if (kb >= max_lo && kb + FK <= min_hi) continue;
+#pragma unroll 1
+        for (int32_t key = max(kb, k0); key < min(kb + FK, k1); ++key) {
+          uint64_t kp, vp;
+          find(key, kp, vp);
+          const bool seen = key < hi && key >= lo;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) o[i][k] = seen ? fmaf(w, v[k], o[i][k]) : o[i][k];
-            }
+          for (int i = 0; i < DT; ++i) {
+            const f32x4 v = four_values<T, KV8>(vp, 16 * i + 4 * grp);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[i][k] = seen && !is_finite(v[k]) ? o[i][k] + v[k] : o[i][k];
           }
-#pragma unroll
-          for (int k = 0; k < 7; ++k) p[k] = p[k + 1];
-        }
-      } else {
-        const u32x4 pw{T::pack(p[0], p[1]), T::pack(p[2], p[3]), T::pack(p[4], p[5]), T::pack(p[6], p[7])};
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-          const int r = 4 * grp + col / 4, c = 2 * i + (col % 4) / 2;
-          const char *x = my + r * (2 * D) + ((c ^ (2 * (r & SWZ))) * 16) + (col & 1) * 8;
-          const u32x2 v0 = read_transposed(x), v1 = read_transposed(x + 16 * (2 * D));  // r + 16: the same exchange
-          o[i] = T::mfma16(u32x4{v0.x, v0.y, v1.x, v1.y}, pw, o[i]);
         }
       }
     }

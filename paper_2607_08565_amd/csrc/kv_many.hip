@@ -212,41 +212,6 @@ __device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, i
   __builtin_amdgcn_s_setprio(0);
 }
 
-// The products where some value is not finite and rows differ in what they see: 0 times it
-// must not reach a row that does not see it.  Rare, so plain sums: weight r of either half.
-template <typename T, int D>
-__device__ __forceinline__ void products_apart(Rows<D> &w, const char *vl, int32_t kb, float sc, int lane,
-                                               f32x16 (&s)[2]) {
-  constexpr int DT = D / 32, ROWB = 2 * D;
-  const int col = lane & 31, half = lane >> 5;
-  const float base = exponent<T>(w);
-  float pair = 0.0f;
-#pragma unroll 1
-  for (int r = 0; r < 32; ++r) {
-    const float x = __builtin_amdgcn_exp2f(fmaf(s[0][0], sc, base));
-    if (r % 2) w.l += pair + x;  // in the order of products()
-    pair = x;
-#pragma unroll 1
-    for (int h = 0; h < 2; ++h) {
-      const float p = __shfl(x, col + 32 * h);
-      const int vrow = 32 * (r / 16) + 8 * (r % 16 / 4) + 4 * h + r % 4, key = kb + vrow;
-      const bool seen = key < w.hi && key >= w.lo;
-#pragma unroll
-      for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {  // components 32 i + 8 g + 4 half + 0 .. 3
-          const u32x2 x2 = *reinterpret_cast<const u32x2 *>(vl + vrow * ROWB + (((4 * i + g) ^ value_swap<D>(vrow)) * 16) +
-                                                            half * 8);
-          const float v[4] = {T::lo(x2.x), T::hi(x2.x), T::lo(x2.y), T::hi(x2.y)};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) w.o[i][4 * g + k] = seen ? fmaf(p, v[k], w.o[i][4 * g + k]) : w.o[i][4 * g + k];
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < 31; ++k) s[k / 16][k % 16] = s[(k + 1) / 16][(k + 1) % 16];
-  }
-}
-
 // Where some row's maximum has grown by more than 2^SLACK: sums scaled down.  The branch
 // around the products is part of the instruction sequence, so that for the compiler the sums
 // are changed in one place and keep their registers; around a branch of its own it keeps
@@ -273,9 +238,9 @@ __device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown
   for (int r = 0; r < 16; ++r) o[r] = x[r];
 }
 
-// A step.  ENDS: not every row sees all of its keys; odd: and some value is not finite.
+// A step.  ENDS: not every row sees all of its keys.
 template <typename T, int D, bool ENDS>
-__device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc, bool odd, int lane) {
+__device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc, int lane) {
   f32x16 s[2];
   Values<D> first;
   const float mx = scores<T, D, ENDS>(w, kl, vl, kb, sc, lane, s, first);
@@ -289,10 +254,7 @@ __device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl,
   }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
-  if (ENDS && odd)
-    products_apart<T>(w, vl, kb, sc, lane, s);
-  else
-    products<T>(w, vl, sc, lane, s, first);
+  products<T>(w, vl, sc, lane, s, first);
 }
 
 // A wavefront's rows: the output, or the sums for the joining.
@@ -333,6 +295,33 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
   }
 }
 
+// What a row sees of a value that is not finite, added to what write_rows has written.  Weights
+// are positive: infinities and NaN come through as they are.  A lane takes the components that it
+// has written.  Rare, and here, where the sums' registers are free, at no cost to the steps.
+template <typename T, bool KV8, int D>
+__device__ __forceinline__ void add_not_finite(const AttendArgs &a, const PlanItem &it, uint64_t value, int32_t kvh, int wave,
+                                               int lane, float vs) {
+  const int col = lane & 31, half = lane >> 5;
+  const int32_t row = it.tile * MANY_ROWS + 32 * wave + col, tok = row / a.group, head = kvh * a.group + row % a.group;
+  const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
+#pragma unroll 1
+  for (int n = 0; n < D / 8; ++n) {
+    const int c = it.part < 0 ? 16 * (n / 2) + 8 * half + 4 * (n % 2) : 8 * n + 4 * half;
+    const f32x4 v = four_values<T, KV8>(value, c);
+    if (is_finite(v[0]) && is_finite(v[1]) && is_finite(v[2]) && is_finite(v[3])) continue;
+    u32x2 *out = reinterpret_cast<u32x2 *>(a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head + c);
+    f32x4 *sum = reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + c);
+    f32x4 x = it.part < 0 ? f32x4{T::lo(out->x), T::hi(out->x), T::lo(out->y), T::hi(out->y)} : *sum;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (!is_finite(v[k])) x[k] += v[k] * vs;
+    if (it.part < 0)
+      *out = u32x2{T::pack(x[0], x[1]), T::pack(x[2], x[3])};
+    else
+      *sum = x;
+  }
+}
+
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
 template <typename T, bool KV8, int D, bool WIDE>
 __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
@@ -345,7 +334,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
   constexpr int ROWB = 2 * D;         // bytes of a row in LDS
   constexpr int SIDE = KT * ROWB;     // bytes of a step's keys, and of its values
   __shared__ __attribute__((aligned(1024))) char lds[4 * SIDE];  // a step's keys, values; the next one's
-  __shared__ int32_t odd_step;  // the last step with a value that is not finite
+  __shared__ int32_t odd_piece;  // the last piece in which look_over has met a value that is not finite
 
   const int32_t kvh = blockIdx.x % a.n_kv, share = blockIdx.x / a.n_kv;
   // asked for together: a workgroup's start is a chain of round trips
@@ -358,6 +347,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
   if (share >= hdr.n_groups) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int col = lane & 31, half = lane >> 5;
+  if (threadIdx.x == 0) odd_piece = -1;  // (a barrier follows before look_over)
   for (int32_t piece = first_piece; piece < last_piece; ++piece) {
     const PlanItem it = uniform(a.items[piece]);
     const int32_t row0 = it.tile * MANY_ROWS + 32 * wave;
@@ -366,7 +356,6 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     const bool too_long = int64_t(it.kv_len) > int64_t(a.cache.max_pages) * a.cache.ps.size;
     const int32_t k0 = uniform(too_long ? 0 : it.k0), k1 = uniform(too_long ? 0 : it.k1);
     if (too_long && threadIdx.x == 0) set_status(a.status, SMETRIC_EINVAL);
-    if (threadIdx.x == 0) odd_step = -1;
 
     Rows<D> w;
     const bool has_row = col < n_rows;
@@ -494,7 +483,8 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
       }
     };
     // A step at the ends of what the rows see: values outside [k0, k1), which may be anything,
-    // become zeros; a value that is not finite marks the step.
+    // become zeros, as do those that are not finite -- 0 times them must not reach a row that does
+    // not see them -- which add_not_finite adds to the rows that do.
     const auto look_over = [&](int32_t kb, char *vl) {
       constexpr int TPR = MT / KT, BYTES = ROWB / TPR;
       const int r = threadIdx.x / TPR;
@@ -503,12 +493,15 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
       bool odd = false;
 #pragma unroll
       for (int i = 0; i < BYTES; i += 16) {
-        if (in)
-          odd |= any_not_finite<T>(*reinterpret_cast<const u32x4 *>(p + i));
-        else
-          *reinterpret_cast<u32x4 *>(p + i) = u32x4{0, 0, 0, 0};
+        u32x4 &x = *reinterpret_cast<u32x4 *>(p + i);
+        if (!in) {
+          x = u32x4{0, 0, 0, 0};
+        } else if (any_not_finite<T>(x)) {
+          x = finite_only<T>(x);
+          odd = true;
+        }
       }
-      if (odd) odd_step = kb;
+      if (odd) odd_piece = piece;
       __syncthreads();
     };
     const auto arrived = [] {
@@ -532,16 +525,15 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
         load_next(kb);
         if (ENDS) look_over(kb, here() + SIDE);
         if (!ENDS || (n_rows > 0 && kb < max_hi && kb + KT > min_lo))
-          step<T, D, ENDS>(w, here(), here() + SIDE, kb, sc, ENDS && odd_step == kb, lane);
+          step<T, D, ENDS>(w, here(), here() + SIDE, kb, sc, lane);
         if (KV8 && kb + KT < k1) to_16(there());
         arrived();
       }
     };
 
-    __syncthreads();  // odd_step is set before a step may mark it
+    // steps that every row of the tile sees whole lie between full0 and full1
+    const int32_t full0 = (max(k0, tile_max_lo) + KT - 1) / KT * KT, full1 = min(k1, tile_min_hi) / KT * KT;
     if (kb0 < k1) {
-      // steps that every row of the tile sees whole lie between full0 and full1
-      const int32_t full0 = (max(k0, tile_max_lo) + KT - 1) / KT * KT, full1 = min(k1, tile_min_hi) / KT * KT;
       if (WIDE) find_steps(kb0);
       load_step(kb0, here());
       if (KV8) to_16(here());
@@ -560,6 +552,16 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     }
     const float vs = KV8 && a.cache.v_scale ? a.cache.v_scale[kvh] : 1.0f;
     write_rows<T>(a, it, w, kvh, wave, again(lane), vs);
+    if (kb0 < k1 && odd_piece == piece) {  // (the next piece's first barrier comes after all have read it)
+#pragma unroll 1
+      for (int32_t key = k0; key < k1; ++key) {
+        if (key >= full0 && key < full1) key = full1;
+        if (key >= k1) break;
+        uint64_t kp, vp;
+        find(key, kp, vp);
+        if (key < w.hi && key >= w.lo) add_not_finite<T, KV8, D>(a, it, vp, kvh, wave, lane, vs);
+      }
+    }
   }
 }
 
