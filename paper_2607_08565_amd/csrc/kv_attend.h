@@ -105,10 +105,9 @@ __device__ __forceinline__ bool plan_fits(const AttendArgs &a, const PlanHdr &h)
          h.dim == a.dim && h.window == a.window && h.n_tokens == a.n_tokens;
 }
 
-// lse from a row's maximum (in powers of two) and sum of weights.
-template <typename T>
-__device__ __forceinline__ float lse_of(float m, float l) {
-  return l == 0.0f ? -INFINITY : (m + (log2f(l) - T::P_SHIFT)) * 0.693147180559945309f;
+// lse from a row's maximum (in powers of two) and sum of weights times 2^shift.
+__device__ __forceinline__ float lse_of(float m, float l, float shift) {
+  return l == 0.0f ? -INFINITY : (m + log2f(l * exp2f(-shift))) * 0.693147180559945309f;
 }
 
 // Launches (one per file).  Grids cover plan_shape's bounds; workgroups past the plan's

@@ -26,7 +26,8 @@ constexpr float E4M3_MAX = 448.0f;
 struct Bf16 {
   typedef bf16x8 V8;
   static constexpr uint32_t EXP = 0x7F807F80u, ONE_EXP = 0x00800080u;  // exponent bits, their lowest (both halves)
-  static constexpr float P_SHIFT = 0.0f;  // weights are held times 2^P_SHIFT
+  // weights are held times a power of two, for few rows and for many (whose maximum may lag by 2^8)
+  static constexpr float FEW_SHIFT = 0.0f, MANY_SHIFT = 0.0f;
   __device__ static __forceinline__ float lo(uint32_t x) { return __uint_as_float(x << 16); }
   __device__ static __forceinline__ float hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
   __device__ static __forceinline__ uint32_t pack(float a, float b) {  // to nearest even, v_cvt_pk_bf16_f32
@@ -47,7 +48,8 @@ struct Bf16 {
 struct F16 {
   typedef f16x8 V8;
   static constexpr uint32_t EXP = 0x7C007C00u, ONE_EXP = 0x04000400u;
-  static constexpr float P_SHIFT = 4.0f;
+  // as large as the type allows (2^15), for it holds weights below 2^-14 with fewer than 11 bits
+  static constexpr float FEW_SHIFT = 15.0f, MANY_SHIFT = 7.0f;
   __device__ static __forceinline__ float lo(uint32_t x) { return float(__builtin_bit_cast(f16x2, x).x); }
   __device__ static __forceinline__ float hi(uint32_t x) { return float(__builtin_bit_cast(f16x2, x).y); }
   __device__ static __forceinline__ uint32_t pack(float a, float b) {

@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] *= down;
       }
-      const float base = (m == -INFINITY ? 0.0f : m) - T::P_SHIFT;
+      const float base = (m == -INFINITY ? 0.0f : m) - T::FEW_SHIFT;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         p[e] = __builtin_amdgcn_exp2f(p[e] - base);
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
         for (int i = 0; i < N; i += 4)
           *reinterpret_cast<u32x2 *>(p + i) =
               u32x2{T::pack(acc[i] * inv, acc[i + 1] * inv), T::pack(acc[i + 2] * inv, acc[i + 3] * inv)};
-        if (a.lse && jc == 0) a.lse[(int64_t(it.tok0) + jt) * a.n_q + jh] = lse_of<T>(mm, ll);
+        if (a.lse && jc == 0) a.lse[(int64_t(it.tok0) + jt) * a.n_q + jh] = lse_of(mm, ll, T::FEW_SHIFT);
       } else {
         const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * FEW_ROWS + jr;
 #pragma unroll

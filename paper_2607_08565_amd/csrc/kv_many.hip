@@ -172,8 +172,8 @@ __device__ __forceinline__ float scores(const Rows<D> &w, const char *kl, const 
   return __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * sc;
 }
 template <typename T, int D>
-__device__ __forceinline__ float exponent(const Rows<D> &w) {  // of weight 2^P_SHIFT
-  return T::P_SHIFT - (w.m == -INFINITY ? 0.0f : w.m);
+__device__ __forceinline__ float exponent(const Rows<D> &w) {  // of weight 2^MANY_SHIFT
+  return T::MANY_SHIFT - (w.m == -INFINITY ? 0.0f : w.m);
 }
 
 // The products of 16 keys' weights with their values, among them the next 16's weights and reads.
@@ -282,7 +282,7 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
         }
         if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
       }
-    if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of<T>(w.m, w.l);
+    if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of(w.m, w.l, T::MANY_SHIFT);
   } else if (has_row) {
     const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
 #pragma unroll

@@ -231,7 +231,7 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
 // many rows at once (each of a few parts).  Tiles of few rows, which may have hundreds of
 // parts: it takes one row's parts side by side.
 constexpr int32_t JOIN_GRID = 2048;
-template <typename T, int D>
+template <typename T, int D, bool FEW>
 __device__ __forceinline__ void write_row(const AttendArgs &a, const PlanSplit &s, int32_t in_req, int32_t kvh, int sub,
                                           f32x4 acc, float m, float l) {
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -239,7 +239,7 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, const PlanSplit &
   const int32_t head = kvh * a.group + in_req % a.group;
   *reinterpret_cast<u32x2 *>(a.out.data + t * a.out.token + head * a.out.head + sub * 4) =
       u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
-  if (a.lse && sub == 0) a.lse[t * a.n_q + head] = lse_of<T>(m, l);
+  if (a.lse && sub == 0) a.lse[t * a.n_q + head] = lse_of(m, l, FEW ? T::FEW_SHIFT : T::MANY_SHIFT);
 }
 template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
         }
       }
     }
-    if (!FEW || side == 0) write_row<T, D>(a, s, in_req, kvh, sub, acc, m, l);
+    if (!FEW || side == 0) write_row<T, D, FEW>(a, s, in_req, kvh, sub, acc, m, l);
     if (FEW) __syncthreads();
   }
 }
