@@ -127,7 +127,10 @@ def append(cache: PagedCache, page_table: torch.Tensor, q_off: torch.Tensor, kv_
 class Plan:
     """How a step's attention is split over the GPU: made once per step from the lengths, used
     by every layer.  The buffers (plan and workspace) are kept; a plan serves any batch of the
-    same n_req and n_tokens after another make()."""
+    same n_req and n_tokens after another make().  They belong to the stream that is current
+    here: work on another one has to end before the plan is dropped, as torch then hands
+    their memory out again.  workspace: a contiguous uint8 tensor of ws_bytes, 256-byte
+    aligned, which plans used in turn on one stream may share."""
 
     def __init__(self, n_req: int, n_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_new: int,
                  window: int = 0, device="cuda", workspace: torch.Tensor | None = None):
@@ -136,9 +139,13 @@ class Plan:
         a, b = C.c_uint64(), C.c_uint64()
         _check("smetric_attend_plan_bytes", _lib.smetric_attend_plan_bytes(*self.args, C.byref(a), C.byref(b)))
         self.plan_bytes, self.ws_bytes = int(a.value), int(b.value)
+        if torch.device(device).type != "cuda":
+            raise TypeError("device: expected a CUDA device")
+        if workspace is not None:
+            _dev(workspace, torch.uint8, "workspace")
+            if workspace.numel() < self.ws_bytes:
+                raise SmetricError("smetric_attend_plan_bytes", EINVAL)
         self.mem = torch.empty(self.plan_bytes, dtype=torch.uint8, device=device)
-        if workspace is not None and workspace.numel() < self.ws_bytes:
-            raise SmetricError("smetric_attend_plan_bytes", EINVAL)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device) if workspace is None else workspace
         self.plan_ptr, self.ws_ptr = self.mem.data_ptr(), self.workspace.data_ptr()
         self.q_off = self.kv_len = None
