@@ -7,7 +7,8 @@ model's layer on a batch of requests, each with one new token or a chunk of them
     q = kv.append(cache, table, q_off, kv_len, k, v, q=q, rotary=rotary)  # per layer
     out = kv.attend(q, cache, table, plan)
 
-Tensors go in by data pointer on torch's current stream; there is no CPU fallback.
+Tensors go in by data pointer on torch's current stream of the current device, which has to be
+theirs; there is no CPU fallback.
 """
 from __future__ import annotations
 
@@ -40,6 +41,14 @@ def _opt(t: torch.Tensor | None, dtype: torch.dtype, name: str):
     return None if t is None else _dev(t, dtype, name)
 
 
+def _device(*tensors: torch.Tensor | None) -> int:
+    """The index of the device that all of them are on, -1 if there are none."""
+    on = {t.get_device() for t in tensors if t is not None}
+    if len(on) > 1:
+        raise ValueError("tensors on different devices")
+    return on.pop() if on else -1
+
+
 class PagedCache:
     """Keys and values in pages: two tensors [n_pages, n_kv_heads, page_size, head_dim] of any
     strides with contiguous components (a view of another order is one), bfloat16, float16
@@ -52,13 +61,14 @@ class PagedCache:
                 raise TypeError(f"{name}: expected a CUDA tensor [pages, heads, page_size, head_dim] of 16 or 8 bits")
             if t.stride(3) != 1:
                 raise ValueError(f"{name}: components must be contiguous")
-        if k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
-            raise ValueError("k and v differ in shape, type or device")
+        if k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v differ in shape or type")
         if (k_scale is None) != (v_scale is None):
             raise ValueError("k_scale and v_scale go together")
         if k_scale is not None and (k.dtype != torch.float8_e4m3fn or k_scale.numel() != k.shape[1] or
                                     v_scale.numel() != k.shape[1]):
             raise ValueError("scales: one per head of a float8_e4m3fn cache")
+        self.device = _device(k, v, k_scale, v_scale)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.dtype = k.dtype
@@ -85,6 +95,7 @@ class Rotary:
         if rot_dim and (table is None or table.dim() != 2 or table.shape[1] != rot_dim):
             raise ValueError(f"table: expected [positions, {rot_dim}]")
         self.table, self.q_weight, self.k_weight, self.rot_dim = table, q_weight, k_weight, rot_dim
+        self.device = _device(table if rot_dim else None, q_weight, k_weight)
         w = [None if x is None else _dev(x, x.dtype, n) for x, n in ((q_weight, "q_weight"), (k_weight, "k_weight"))]
         self.c = _Rotary(w[0], w[1], _opt(table, torch.float32, "table") if rot_dim else None,
                          table.shape[0] if rot_dim else 0, rot_dim, int(interleaved), eps)
@@ -103,7 +114,8 @@ def qk_rotate(q: torch.Tensor, k: torch.Tensor, rotary: Rotary, positions: torch
     their positions (int32).  Outputs may be the inputs.  Returns (q_out, k_out)."""
     q_out = _new(q, "q") if q_out is None else q_out
     k_out = _new(k, "k") if k_out is None else k_out
-    rc = _kv_calls.qk_rotate(q, k, rotary.ref, rotary.q_weight, rotary.k_weight, positions, q_out, k_out, status)
+    rc = _kv_calls.qk_rotate(q, k, rotary.ref, rotary.q_weight, rotary.k_weight, positions, q_out, k_out, status,
+                            rotary.device)
     if rc:
         raise SmetricError("smetric_qk_rotate", rc)
     return q_out, k_out
@@ -118,7 +130,8 @@ def append(cache: PagedCache, page_table: torch.Tensor, q_off: torch.Tensor, kv_
     if q is not None and q_out is None:
         q_out = _new(q, "q")
     r = (0, None, None) if rotary is None else (rotary.ref, rotary.q_weight, rotary.k_weight)
-    rc = _kv_calls.append(cache.ref, page_table, q_off, kv_len, k, v, q, q_out, *r, positions, status)
+    rc = _kv_calls.append(cache.ref, page_table, q_off, kv_len, k, v, q, q_out, *r, positions, status, cache.device,
+                          -1 if rotary is None else rotary.device)
     if rc:
         raise SmetricError("smetric_kv_append", rc)
     return q_out if q is not None else None
@@ -147,12 +160,14 @@ class Plan:
                 raise SmetricError("smetric_attend_plan_bytes", EINVAL)
         self.mem = torch.empty(self.plan_bytes, dtype=torch.uint8, device=device)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device) if workspace is None else workspace
+        self.device = _device(self.mem, self.workspace)
         self.plan_ptr, self.ws_ptr = self.mem.data_ptr(), self.workspace.data_ptr()
         self.q_off = self.kv_len = None
 
     def make(self, q_off: torch.Tensor, kv_len: torch.Tensor, status: torch.Tensor | None = None) -> "Plan":
         """smetric_attend_plan for these lengths (device tensors, read on the current stream)."""
-        rc = _kv_calls.make_plan(q_off, kv_len, *self.args, self.window, self.plan_ptr, self.plan_bytes, status)
+        rc = _kv_calls.make_plan(q_off, kv_len, *self.args, self.window, self.plan_ptr, self.plan_bytes, status,
+                                 self.device)
         if rc:
             raise SmetricError("smetric_attend_plan", rc)
         self.q_off, self.kv_len = q_off, kv_len
@@ -172,7 +187,7 @@ def attend(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, plan: P
     out = _new(q, "q") if out is None else out
     rc = _kv_calls.attend(q, out, lse, cache.ref, page_table, plan.q_off, plan.kv_len, T, Hq,
                           D ** -0.5 if scale is None else scale, max_new, plan.window, plan.plan_ptr, plan.plan_bytes,
-                          plan.ws_ptr, plan.ws_bytes, status)
+                          plan.ws_ptr, plan.ws_bytes, status, cache.device, plan.device)
     if rc:
         raise SmetricError("smetric_attend", rc)
     return out

@@ -23,3 +23,51 @@ def test_plan_takes_device_memory_only():
                 kv.Plan(*SHAPE, workspace=w)
         with pytest.raises(SmetricError):
             kv.Plan(*SHAPE, workspace=u8(16))
+
+
+def _args(on):
+    """A call's tensors by name, on cuda:0 or, where `on` names them, on cuda:1."""
+    dev = lambda name: "cuda:1" if name == on else "cuda:0"  # noqa: E731
+    bf = lambda name, *s: torch.empty(s, dtype=torch.bfloat16, device=dev(name))  # noqa: E731
+    num = lambda name, t, *s: torch.empty(s, dtype=t, device=dev(name))  # noqa: E731
+    return dict(q=bf("q", 3, 4, 64), k=bf("k", 3, 2, 64), v=bf("v", 3, 2, 64), out=bf("out", 3, 4, 64), k_out=bf("k_out", 3, 2, 64),
+                table=num("table", torch.int32, 2, 4), q_off=num("q_off", torch.int64, 3), kv_len=num("kv_len", torch.int32, 2),
+                positions=num("positions", torch.int32, 3), status=num("status", torch.int32, 1),
+                lse=num("lse", torch.float32, 3, 4), cache=kv.PagedCache(*[bf("cache", 5, 2, 16, 64) for _ in "kv"]),
+                rotary=kv.Rotary(num("rotary", torch.float32, 8, 64)), plan=kv.Plan(*SHAPE, device=dev("plan")))
+
+
+def _calls(x):
+    p = x["plan"]
+    return dict(
+        rotate=(("q", "k", "rotary", "positions", "out", "k_out", "status"),
+                lambda: kv.qk_rotate(x["q"], x["k"], x["rotary"], x["positions"], x["out"], x["k_out"], x["status"])),
+        append=(("cache", "table", "q_off", "kv_len", "k", "v", "q", "out", "rotary", "positions", "status"),
+                lambda: kv.append(x["cache"], x["table"], x["q_off"], x["kv_len"], x["k"], x["v"], x["q"], x["out"], x["rotary"],
+                                  x["positions"], x["status"])),
+        make=(("plan", "q_off", "kv_len", "status"), lambda: p.make(x["q_off"], x["kv_len"], x["status"])),
+        attend=(("q", "cache", "table", "plan", "out", "lse", "q_off", "kv_len", "status"),
+                lambda: kv.attend(x["q"], x["cache"], x["table"], p, out=x["out"], lse=x["lse"], status=x["status"])))
+
+
+@pytest.mark.parametrize("call", ["rotate", "append", "make", "attend"])
+def test_tensors_of_another_device(call):
+    """One tensor, cache, table of angles or plan of another device than the others is refused."""
+    if torch.cuda.is_available() and torch.cuda.device_count() < 2:
+        pytest.skip("torch makes no stand-in for a second device beside a single real one")
+    with FakeTensorMode():
+        names = _calls(_args(None))[call][0]
+        for name in names:
+            x = _args(name)
+            x["plan"].q_off, x["plan"].kv_len = x["q_off"], x["kv_len"]
+            with pytest.raises(ValueError, match="device"):
+                _calls(x)[call][1]()
+        z = torch.empty(5, 2, 16, 64, dtype=torch.float8_e4m3fn, device="cuda:0")
+        one = lambda d: torch.empty(2, device=d)  # noqa: E731
+        for t in ((z, z.to("cuda:1")), (z, z, one("cuda:1"), one("cuda:0")), (z, z, one("cuda:1"), one("cuda:1"))):
+            with pytest.raises(ValueError, match="device"):
+                kv.PagedCache(*t)
+        with pytest.raises(ValueError, match="device"):
+            kv.Rotary(torch.empty(8, 64, device="cuda:1"), q_weight=torch.empty(64, device="cuda:0"))
+        with pytest.raises(ValueError, match="device"):
+            kv.Plan(*SHAPE, device="cuda:0", workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda:1"))
