@@ -37,26 +37,34 @@ __device__ __forceinline__ u32x2 swap32(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
 }
 
-// 64 lanes' 16 bytes from memory to 1 KB of LDS, past the registers.  The instruction has no
-// output the compiler could take for written; what waits for it is arrived().  (With the
-// compiler's builtin, every later read of LDS waits for it, since both buffers are one
-// array to the alias analysis.)  The waits are those that the hardware leaves to the program,
-// where the compiler does not see into these lines: one instruction between the write of M0
-// and the load, and five between a vector instruction that writes a scalar register, as
-// read_lane does, and a load that reads it.
-__device__ __forceinline__ void to_lds(uint64_t base, uint32_t offset, char *to) {
-  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)to));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2"
-               :
-               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base)
-               : "memory", "m0");
+// Two times 64 lanes' 16 bytes, of keys and of values, from memory to 1 KB of LDS each, past the
+// registers.  The instructions have no output the compiler could take for written; what waits for
+// them is arrived().  (With the compiler's builtin, every later read of LDS waits for it, since
+// both buffers are one array to the alias analysis.)  M0, which says where in LDS, is the
+// compiler's: it is put back.  The waits are those that the hardware leaves to the program, where
+// the compiler does not see into these lines: one instruction between a write of M0 and its load,
+// and five between a vector instruction that writes a scalar register, as read_lane does, and a
+// load that reads it.
+__device__ __forceinline__ uint32_t lds_address(char *p) {
+  return __builtin_amdgcn_readfirstlane(uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)p)));
 }
-__device__ __forceinline__ void to_lds(uint64_t from, char *to) {
-  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)to));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-               :
-               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from)
-               : "memory", "m0");
+__device__ __forceinline__ void to_lds(uint64_t k, uint32_t k_offset, char *k_to, uint64_t v, uint32_t v_offset, char *v_to) {
+  uint32_t kept;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %6\n\ts_mov_b32 m0, %0"
+      : "=&s"(kept)
+      : "s"(lds_address(k_to)), "v"(k_offset), "s"(k), "s"(lds_address(v_to)), "v"(v_offset), "s"(v)
+      : "memory");
+}
+__device__ __forceinline__ void to_lds(uint64_t k, char *k_to, uint64_t v, char *v_to) {
+  uint32_t kept;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\t"
+      "s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, off\n\ts_mov_b32 m0, %0"
+      : "=&s"(kept)
+      : "s"(lds_address(k_to)), "v"(k), "s"(lds_address(v_to)), "v"(v)
+      : "memory");
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {  // one instruction; NaN stays
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
@@ -456,11 +464,9 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
           kr[i] = *reinterpret_cast<const u32x4 *>(kp + ko);
           vr[i] = *reinterpret_cast<const u32x4 *>(vp + vo);
         } else if (WIDE) {
-          to_lds(kp, ko, kl + r * ROWB);
-          to_lds(vp, vo, vl + r * ROWB);
+          to_lds(kp, ko, kl + r * ROWB, vp, vo, vl + r * ROWB);
         } else {
-          to_lds(kp + ko, kl + r * ROWB);
-          to_lds(vp + vo, vl + r * ROWB);
+          to_lds(kp + ko, kl + r * ROWB, vp + vo, vl + r * ROWB);
         }
       }
     };
