@@ -108,7 +108,7 @@ int smetric_qk_rotate(int32_t dtype, int32_t head_dim, int64_t n_tokens, const s
  *   positions  int32[n_tokens] or NULL: a token's place in its request is its position
  * A padding token writes nothing to the cache and zeros to q_out; so does one with a bad
  * input (an inconsistent request, page or position), which also sets status.  E4M3 pages
- * hold x / scale rounded to nearest even, saturated at 448 (NaN stays NaN).  Tokens that
+ * hold x / scale rounded to nearest even, saturated at 448 (NaN, also that of 0 / 0, stays NaN).  Tokens that
  * share a place race; pages shared by requests may be read but not appended to.
  * Host errors: EINVAL. */
 int smetric_kv_append(int32_t dtype, const smetric_kv_cache *cache /* host */, const smetric_batch *batch /* host */,
@@ -123,9 +123,10 @@ int smetric_kv_append(int32_t dtype, const smetric_kv_cache *cache /* host */, c
  * j <= p and, with window > 0, j > p - window:
  *   s_j = scale (q . k_j),  out = sum_j exp(s_j - lse) v_j,  lse = log(sum_j exp(s_j))
  * and out = 0, lse = -inf when it sees nothing.  Scores, maxima, sums and the output are
- * held in float32; exp(s_j - m) is rounded to the activations' type for the product with
- * the values.  Tokens that a row does not see change nothing in it, whatever they hold; nor
- * does what a page holds past kv_len.  Splits are joined in a fixed order, so the same call
+ * held in float32; exp(s_j - m), with m the largest score so far or at most log(2^8) below it, is
+ * rounded to the activations' type for the product with the values (F16 loses bits of those below
+ * 2^-21 of the largest, BF16 holds 8 of any).  Tokens that a row does not see change not a bit of
+ * it, whatever they hold; nor does what a page holds past kv_len.  Splits are joined in a fixed order, so the same call
  * gives the same bits.
  *
  * The plan holds how the batch's rows and cached tokens are split into pieces of work.  It

@@ -40,7 +40,7 @@ static_assert(sizeof(PlanHdr) == 128 && sizeof(PlanItem) == 32 && sizeof(PlanSpl
 // compute units two, one with heads of 256: their registers), each with an equal share of the
 // key steps in order, so that all end together; a share begins and ends within a tile, which is
 // then in pieces, and may hold several tiles.  Heads of 64 would leave room for three, which is
-// no faster (4 chunks of 2,048 over 8-bit pages: 740 us, with two 702); heads of 256 with twice
+// no faster (4 chunks of 2,048 over 8-bit pages: 732 us, with two 694); heads of 256 with twice
 // as many shares as run at once: 2 chunks of 2,048 910 us for 858, 65,536 keys 59 for 53.
 // Two exceptions: no share is smaller than MIN_STEPS, and a cut this near a tile's end goes to
 // the end (EDGE_STEPS).  Few rows: a step is half a block of each wavefront, so two make the

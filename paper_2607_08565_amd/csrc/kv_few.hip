@@ -12,10 +12,11 @@
 // formed as S^T = K Q^T: a lane then holds scores of one row only, its maximum takes two
 // lane exchanges, and the weights are where the second product, O^T = V^T P^T, wants them:
 // its order of keys is free as long as both operands use one, so the order in which S^T
-// leaves them is used.  The next 32 keys' loads are in flight during all of it.
+// leaves them is used.  The next 32 keys' loads are in flight during all of it.  Weights are rounded
+// to the activations' type for it, as the matrix cores take 16-bit operands; their sum is not.
 //
-// Measured: 32 requests decoding over 1.73 GB of cache 303 us, 5.7 TB/s (a copy of 4 GiB moves
-// 4.8); 64 drafted tokens over 0.58 GB 115 us; 131,072 keys of 8 bits (134 MB) 31 to 35 us, 24
+// Measured: 32 requests decoding over 1.73 GB of cache 305 us, 5.7 TB/s (a copy of 4 GiB moves
+// 4.8); 64 drafted tokens over 0.58 GB 117 us; 131,072 keys of 8 bits (134 MB) 31 to 35 us, 24
 // of them here and the rest the joining; a lone token over 1,025 keys 9.5 us, two launches.
 #include <math.h>
 

@@ -12,14 +12,16 @@
 // The products are S^T = K Q^T and O^T = V^T P^T: a lane holds scores of one row only, so its
 // maximum takes one lane exchange, and its weights are where the second product wants them --
 // the order in which S^T leaves the keys is the order in which V^T is read, transposed, from LDS.
+// Weights are rounded to the activations' type for it, as the matrix cores take 16-bit operands;
+// their sum is not.
 //
-// Measured: 4,096 tokens over 16,384 (32 heads of 128) 941 to 990 us from card to card, 1,020 TFLOP/s; the library's product
-// of matrices of 16,384 reaches 1,340, of 8,192 1,130.  The matrix cores work half of the cycles
+// Measured: 4,096 tokens over 16,384 (32 heads of 128) 923 to 986 us, 1,041 to 976 TFLOP/s, from card to card; on the
+// faster one the library's product of matrices of 16,384 reaches 1,402, of 8,192 1,173.  The matrix cores work half of the cycles
 // and the vector instructions about as long (33 exponentials, 32 sums, 31 products and 16
 // maxima a step of 32 matrix instructions), on two wavefronts that overlap them in part, at a
 // clock that falls under the load (1.9 GHz).  With the keys always in the nearest cache it takes
 // 5 % less, without the exponentials 8 %, without the maximum 5 %.  Heads of 64 do half the
-// products for the same weights: 24 requests with up to 1,000 new tokens 113 us, 366 TFLOP/s.
+// products for the same weights: 24 requests with up to 1,000 new tokens 108 to 112 us, 370 to 383 TFLOP/s.
 #include <math.h>
 
 #include <type_traits>
@@ -226,6 +228,8 @@ __device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, i
 // them twice, which leaves no room for keys and values read ahead.  The products of the
 // step before are long done: this step's scores, which came after them, have been read.  The
 // next product may read what was scaled two instructions later, hence the wait at the end.
+// (Heads of 256: the sums live in accumulation registers, and the operands here are vector ones, so
+// that each step moves 128 sums here and back, besides 32 scores, for its 64 products.)
 __device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown) {
   float x[16];
 #pragma unroll
