@@ -68,7 +68,6 @@ class PagedCache:
         if k_scale is not None and (k.dtype != torch.float8_e4m3fn or k_scale.numel() != k.shape[1] or
                                     v_scale.numel() != k.shape[1]):
             raise ValueError("scales: one per head of a float8_e4m3fn cache")
-        self.device = _device(k, v, k_scale, v_scale)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.dtype = k.dtype
@@ -76,6 +75,7 @@ class PagedCache:
                         (C.c_int64 * 3)(*v.stride()[:3]), self.page_size, self.n_kv_heads, self.head_dim,
                         _DTYPES[k.dtype], _opt(k_scale, torch.float32, "k_scale"),
                         _opt(v_scale, torch.float32, "v_scale"))
+        self.device = _device(k, v, k_scale, v_scale)
         self.ref = C.addressof(self.c)
 
     @classmethod
@@ -95,10 +95,10 @@ class Rotary:
         if rot_dim and (table is None or table.dim() != 2 or table.shape[1] != rot_dim):
             raise ValueError(f"table: expected [positions, {rot_dim}]")
         self.table, self.q_weight, self.k_weight, self.rot_dim = table, q_weight, k_weight, rot_dim
-        self.device = _device(table if rot_dim else None, q_weight, k_weight)
         w = [None if x is None else _dev(x, x.dtype, n) for x, n in ((q_weight, "q_weight"), (k_weight, "k_weight"))]
         self.c = _Rotary(w[0], w[1], _opt(table, torch.float32, "table") if rot_dim else None,
                          table.shape[0] if rot_dim else 0, rot_dim, int(interleaved), eps)
+        self.device = _device(table if rot_dim else None, q_weight, k_weight)
         self.ref = C.addressof(self.c)
 
 

@@ -71,3 +71,17 @@ def test_tensors_of_another_device(call):
             kv.Rotary(torch.empty(8, 64, device="cuda:1"), q_weight=torch.empty(64, device="cuda:0"))
         with pytest.raises(ValueError, match="device"):
             kv.Plan(*SHAPE, device="cuda:0", workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda:1"))
+
+
+def test_host_memory_is_another_type():
+    """A host tensor is a TypeError also beside device tensors."""
+    with FakeTensorMode():
+        t, w = torch.empty(8, 64, device="cuda"), torch.empty(64, device="cuda")
+        for args in (dict(table=t.cpu()), dict(table=t, q_weight=w.cpu()), dict(table=t.cpu(), k_weight=w)):
+            with pytest.raises(TypeError):
+                kv.Rotary(**args)
+        z = torch.empty(5, 2, 16, 64, dtype=torch.float8_e4m3fn, device="cuda")
+        s = torch.empty(2, device="cuda")
+        for args in ((z, z.cpu()), (z, z, s, s.cpu()), (z, z, s.cpu(), s.cpu())):
+            with pytest.raises(TypeError):
+                kv.PagedCache(*args)
