@@ -72,9 +72,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // one instr
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
-// A row is scaled down only when its maximum has grown by more than 2^SLACK: until then its
-// weights are at most 2^SLACK instead of 1, which costs no precision, and most steps of a
-// long request leave the sums alone.
+// A row is scaled down only when its own maximum has grown by more than 2^SLACK: until then its
+// weights are at most 2^SLACK instead of 1, which costs BF16 no precision and F16 that many of the
+// powers of two below 1 (MANY_SHIFT), and most steps of a long request leave the sums alone.
 constexpr float SLACK = 8.0f;
 
 // Where a row's 16-byte pieces are in LDS: piece c at c ^ key_swap(row), c ^ value_swap(row).  A
