@@ -10,8 +10,10 @@
  * to be checked) or thousands (a prompt's chunk), mixed as they come:
  *   smetric_qk_rotate     queries and keys normed per head and rotated to their positions
  *   smetric_kv_append     the same with the keys and the values entered into the pages
+ *   smetric_kv_read       cached tokens read back as activations
  *   smetric_attend_plan   how a step's attention is split over the GPU (once per step)
  *   smetric_attend        the attention of the new tokens over the pages (once per layer)
+ *   smetric_attend_scores the same with capped scores, or a bias by distance
  *
  * Conventions are those of smetric.h: device pointers unless marked (host), no allocation,
  * work enqueued on `stream`, host-visible errors returned with nothing enqueued, and errors
@@ -27,9 +29,13 @@
 extern "C" {
 #endif
 
-/* Element types.  Activations are BF16 or F16; a cache has the activations' type or E4M3
- * (the 8-bit float without infinities, largest value 448) with one scale per head. */
-enum { SMETRIC_BF16 = 0, SMETRIC_F16 = 1, SMETRIC_E4M3 = 2 };
+/* Element types.  Activations are BF16 or F16; a cache has the activations' type or
+ *   E4M3  the 8-bit float without infinities, largest value 448, with one scale per head
+ *   E2M1  the 4-bit float +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} (codes 0 .. 7, 8 for the sign), two in a
+ *         byte, the even component in the lower half, and for every 32 neighbouring components of a
+ *         head's token an exponent byte e: a stored x stands for x 2^(e - 127), for NaN where e
+ *         is 255.  4.25 bits a component. */
+enum { SMETRIC_BF16 = 0, SMETRIC_F16 = 1, SMETRIC_E4M3 = 2, SMETRIC_E2M1 = 3 };
 
 /* An activation of shape [n_tokens, heads, head_dim]: components are contiguous, tokens and
  * heads any number of elements apart that keeps every head 16-byte aligned (a slice of a
@@ -39,6 +45,14 @@ typedef struct smetric_heads {
   int64_t token_stride, head_stride; /* elements, multiples of 8 */
 } smetric_heads;
 
+/* The exponent bytes of E2M1 pages: that of components 32 g .. 32 g + 31 of (page, head, token) is
+ * k[page * k_stride[0] + head * k_stride[1] + token * k_stride[2] + g].  A page's keys' and values'
+ * exponents of a head beside each other fill whole lines of memory ([page][head][k, v][token][g]). */
+typedef struct smetric_kv_exps {
+  uint8_t *k, *v;                    /* aligned to head_dim / 32 bytes */
+  int64_t k_stride[3], v_stride[3];  /* bytes, >= 0; multiples of head_dim / 32 */
+} smetric_kv_exps;
+
 /* A paged cache: keys and values of n_pages pages of page_size tokens.  Element (page, head,
  * token, component) of the keys is k[page * k_stride[0] + head * k_stride[1] + token *
  * k_stride[2] + component]; [page][head][token] order keeps what one head reads of a page in
@@ -46,12 +60,13 @@ typedef struct smetric_heads {
 typedef struct smetric_kv_cache {
   void *k, *v;                       /* 16-byte aligned */
   int64_t n_pages;                   /* in [1, 2^31) */
-  int64_t k_stride[3], v_stride[3];  /* elements, >= 0; multiples of 8 (E4M3: 16) */
+  int64_t k_stride[3], v_stride[3];  /* elements, >= 0; multiples of 8 (E4M3: 16, E2M1: 32) */
   int32_t page_size;                 /* tokens, in [1, 65536] */
   int32_t n_kv_heads;
   int32_t head_dim;                  /* 64, 128 or 256 */
   int32_t dtype;
   const float *k_scale, *v_scale;    /* float32[n_kv_heads], E4M3: a stored x stands for x * scale, any number */
+  const smetric_kv_exps *exps;       /* (host) E2M1; not read for other types */
 } smetric_kv_cache;
 
 /* A ragged batch: request r's new tokens are q_off[r] .. q_off[r+1] of the activations and
@@ -108,7 +123,12 @@ int smetric_qk_rotate(int32_t dtype, int32_t head_dim, int64_t n_tokens, const s
  *   positions  int32[n_tokens] or NULL: a token's place in its request is its position
  * A padding token writes nothing to the cache and zeros to q_out; so does one with a bad
  * input (an inconsistent request, page or position), which also sets status.  E4M3 pages
- * hold x / scale rounded to nearest even, saturated at 448 (NaN, also that of 0 / 0, stays NaN).  Tokens that
+ * hold x / scale rounded to nearest even, saturated at 448 (NaN, also that of 0 / 0, stays NaN).
+ * E2M1 pages: 32 components whose largest magnitude is a get e = 127 + k for the smallest k with
+ * a <= 7 2^k, in [-125, 125] (F16: [-23, 13]), where the activations' type holds what the codes stand
+ * for exactly; x / 2^k is rounded to the nearest code, of two equally near ones to the even one, and
+ * saturated at 6, so that no component is further from what it becomes than half of the largest step
+ * (bar what F16 keeps in range); a NaN among the 32 makes e 255, all 32 NaN.  Tokens that
  * share a place race; pages shared by requests may be read but not appended to.
  * Host errors: EINVAL. */
 int smetric_kv_append(int32_t dtype, const smetric_kv_cache *cache /* host */, const smetric_batch *batch /* host */,
@@ -116,6 +136,17 @@ int smetric_kv_append(int32_t dtype, const smetric_kv_cache *cache /* host */, c
                       const smetric_heads *q /* host */, const smetric_heads *q_out /* host */,
                       const smetric_heads *k /* host */, const smetric_heads *v /* host */, int32_t *status,
                       hipStream_t stream);
+
+/* Cached tokens read back: row i of request r of k_out and v_out ([n_tokens, n_kv_heads,
+ * head_dim] of type `dtype`) is place kv_len[r] - (q_off[r+1] - q_off[r]) + i of the request, as
+ * of the new tokens of a step; a whole session's tokens are q_off[r+1] - q_off[r] = kv_len[r].
+ * 16-bit pages are copied bit for bit, 8- and 4-bit values times their scale or power of two in
+ * float32, rounded once.  Rows of padding are zeros; so are those of a bad input (an inconsistent
+ * request or page), which also sets status.  NULL for k_out or v_out leaves that side out.
+ * Host errors: EINVAL. */
+int smetric_kv_read(int32_t dtype, const smetric_kv_cache *cache /* host */, const smetric_batch *batch /* host */,
+                    const smetric_heads *k_out /* host */, const smetric_heads *v_out /* host */, int32_t *status,
+                    hipStream_t stream);
 
 /* ---------------------------------------------------------------------------------
  * Attention of the new tokens over the cache.  Query head h reads key-value head
@@ -125,7 +156,8 @@ int smetric_kv_append(int32_t dtype, const smetric_kv_cache *cache /* host */, c
  * and out = 0, lse = -inf when it sees nothing.  Scores, maxima, sums and the output are
  * held in float32; exp(s_j - m), with m the largest score so far or at most log(2^8) below it, is
  * rounded to the activations' type for the product with the values (F16 loses bits of those below
- * 2^-21 of the largest, BF16 holds 8 of any).  Tokens that a row does not see change not a bit of
+ * 2^-21 of the largest, BF16 holds 8 of any).  What E2M1 pages hold is rounded to the activations' type
+ * first: exact for what smetric_kv_append enters.  Tokens that a row does not see change not a bit of
  * it, whatever they hold; nor does what a page holds past kv_len.  Splits are joined in a fixed order, so the same call
  * gives the same bits.
  *
@@ -154,6 +186,23 @@ int smetric_attend(int32_t dtype, const smetric_kv_cache *cache /* host */, cons
                    int32_t n_q_heads, const smetric_heads *q /* host */, const smetric_heads *out /* host */,
                    float *lse, float scale, int32_t max_new, int32_t window, const void *plan, uint64_t plan_bytes,
                    void *workspace, uint64_t ws_bytes, int32_t *status, hipStream_t stream);
+
+/* The same attention with other scores: for query head h and a token at place p
+ *   s_j = cap tanh(scale (q . k_j) / cap) + slopes[h] (j - p)
+ * The plan is smetric_attend_plan's.
+ *   cap     0: scores as they are; else a number in [2^-20, 2^20]
+ *   slopes  float32[n_q_heads], finite, of either sign, or NULL: no bias
+ * Scores are float32's: a cap's are off by some 2^-23 cap, a bias by 2^-23 of itself.
+ * Host errors: smetric_attend's, and EINVAL for another cap. */
+typedef struct smetric_scores {
+  float cap;
+  const float *slopes;
+} smetric_scores;
+int smetric_attend_scores(int32_t dtype, const smetric_kv_cache *cache /* host */, const smetric_batch *batch /* host */,
+                          int32_t n_q_heads, const smetric_heads *q /* host */, const smetric_heads *out /* host */,
+                          float *lse, float scale, const smetric_scores *scores /* host */, int32_t max_new, int32_t window,
+                          const void *plan, uint64_t plan_bytes, void *workspace, uint64_t ws_bytes, int32_t *status,
+                          hipStream_t stream);
 
 #ifdef __cplusplus
 }

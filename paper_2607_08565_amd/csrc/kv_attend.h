@@ -98,6 +98,8 @@ struct AttendArgs {
   int32_t n_req, n_q, n_kv, group;  // group = n_q / n_kv
   int32_t rows, dim, window;
   float scale_log2;  // scale * log2(e)
+  float cap_log2;    // cap * log2(e), 0: scores are not capped
+  const float *slopes;  // of the query heads, or NULL
   int32_t *status;
 };
 __device__ __forceinline__ bool plan_fits(const AttendArgs &a, const PlanHdr &h) {
@@ -110,10 +112,60 @@ __device__ __forceinline__ float lse_of(float m, float l, float shift) {
   return l == 0.0f ? -INFINITY : (m + log2f(l * exp2f(-shift))) * 0.693147180559945309f;
 }
 
-// Launches (one per file).  Grids cover plan_shape's bounds; workgroups past the plan's
-// counts end at once.
-int launch_few(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_groups, hipStream_t stream);
-int launch_many(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+// Launches (one per file; those of other scores apart).  Grids cover plan_shape's bounds;
+// workgroups past the plan's counts end at once.
+int launch_few(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+int launch_many(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+int launch_few_scores(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+int launch_many_scores(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+
+// Where a place's keys and values are in memory, and the exponents of E2M1 pages.
+struct Place {
+  uint64_t k, v, k_exp, v_exp;
+};
+// A page outside the cache is page 0; returns whether it is one.
+template <Pages KV>
+__device__ __forceinline__ bool find_place(const AttendArgs &a, const int32_t *table, int32_t kvh, int32_t key, Place &p) {
+  const int32_t page = page_of(a.cache.ps, key);
+  int32_t id = table[page];
+  const bool outside = uint32_t(id) >= uint32_t(a.cache.n_pages);
+  if (outside) id = 0;
+  const int32_t slot = key - page * a.cache.ps.size;
+  const auto at = [&](const PageSide &s) {
+    return reinterpret_cast<uint64_t>(s.base + kvh * s.head) + id * s.page + slot * s.token;
+  };
+  p.k = at(a.cache.k);
+  p.v = at(a.cache.v);
+  if (KV == PAGES4) {
+    p.k_exp = at(a.cache.k_exp);
+    p.v_exp = at(a.cache.v_exp);
+  }
+  return outside;
+}
+
+// What a lane takes of a row of E2M1 at once: 16 bytes, a group with one exponent; of the 32 bytes of
+// a head of 64 half a group, so that 16 rows are a wavefront's load as with the others.
+constexpr int piece4(int head_dim) { return head_dim == 64 ? 8 : 16; }
+template <int BYTES>
+__device__ __forceinline__ u32x4 load_piece(uint64_t p) {
+  if (BYTES == 16) return *reinterpret_cast<const u32x4 *>(p);
+  const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+  return u32x4{x.x, x.y, 0, 0};
+}
+__device__ __forceinline__ uint32_t load_exp(uint64_t p) { return *reinterpret_cast<const uint8_t *>(p); }
+
+// Other scores (smetric_attend_scores), in powers of two: of x = q . k, sc = scale log2(e) (and the keys'
+// scale), the capped score, cap tanh(scale x / cap) = cap - 2 cap / (1 + exp(2 scale x / cap)): both ends
+// come out of the exponential's own overflow to infinity and underflow to zero.
+struct Capped {
+  float rate, cap;  // of the exponent, 2 sc / cap; cap log2(e)
+  __device__ __forceinline__ Capped(const AttendArgs &a, float sc)
+      : rate(a.cap_log2 > 0.0f ? 2.8853900817779268f * sc / a.cap_log2 : 0.0f), cap(a.cap_log2) {}
+  __device__ __forceinline__ float operator()(float x) const {
+    return fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * rate)), cap);
+  }
+};
+constexpr float LOG2E = 1.4426950408889634f;
 
 // Whether one of eight 16-bit floats is infinite or NaN: its exponent is all ones, and adding
 // the exponent's lowest bit to the exponent alone carries into the (cleared) sign bit.
@@ -134,14 +186,18 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 x) {
 }
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
 // Components c .. c + 3 of a row of values in memory.
-template <typename T, bool KV8>
-__device__ __forceinline__ f32x4 four_values(uint64_t row, int c) {
+template <typename T, Pages KV>
+__device__ __forceinline__ f32x4 four_values(const Place &p, int c) {
   u32x2 x;
-  if (KV8) {
-    const uint32_t y = *reinterpret_cast<const uint32_t *>(row + c);
+  if (KV == PAGES4) {
+    const uint32_t y = *reinterpret_cast<const uint16_t *>(p.v + c / 2);
+    const float e = power_of(load_exp(p.v_exp + c / GROUP4));
+    x = u32x2{T::template from_e2m1<0>(y, e), T::template from_e2m1<1>(y, e)};
+  } else if (KV == PAGES8) {
+    const uint32_t y = *reinterpret_cast<const uint32_t *>(p.v + c);
     x = u32x2{T::template from_e4m3<false>(y), T::template from_e4m3<true>(y)};
   } else {
-    x = *reinterpret_cast<const u32x2 *>(row + 2 * c);
+    x = *reinterpret_cast<const u32x2 *>(p.v + 2 * c);
   }
   return f32x4{T::lo(x.x), T::hi(x.x), T::lo(x.y), T::hi(x.y)};
 }

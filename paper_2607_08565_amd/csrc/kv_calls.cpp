@@ -224,6 +224,22 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// (cache's address, page_table, q_off, kv_len, k_out, v_out, status, cache's device)
+PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 8, [&] {
+    Device d;
+    same_device(d, a[7], "cache");
+    const auto *cache = address<const smetric_kv_cache>(a[0]);
+    const at::ScalarType type = activations(a[4], "k_out");
+    const Heads k = heads(d, a[4], type, "k_out", -1, cache->n_kv_heads, cache->head_dim);
+    const Heads v = heads(d, a[5], type, "v_out", k.tokens, k.heads, k.dim);
+    const smetric_batch batch = batch_of(d, a[1], a[2], a[3], k.tokens);
+    int32_t *status = array<int32_t>(d, a[6], at::kInt, "status");
+    const hipStream_t s = stream(d);
+    return unlocked([&] { return smetric_kv_read(code_of(type), cache, &batch, &k, &v, status, s); });
+  });
+}
+
 // (q_off, kv_len, n_req, n_tokens, n_q_heads, n_kv_heads, head_dim, max_new, window, plan's
 // address, bytes, status, plan's device)
 PyObject *make_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -249,9 +265,9 @@ PyObject *make_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 // (q, out, lse, cache's address, page_table, q_off, kv_len, n_tokens, n_q_heads, scale, max_new, window, plan's
-// address, bytes, workspace's address, bytes, status, cache's device, plan's)
+// address, bytes, workspace's address, bytes, status, cache's device, plan's, cap, slopes)
 PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return guarded(n, 19, [&] {
+  return guarded(n, 21, [&] {
     Device d;
     same_device(d, a[17], "cache");
     same_device(d, a[18], "plan");
@@ -268,8 +284,11 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
         refuse(PyExc_ValueError, "%s: expected one per token and query head", "lse");
     }
     const smetric_batch batch = batch_of(d, a[4], a[5], a[6], tokens);
-    const double scale = PyFloat_AsDouble(a[9]);
-    if (scale == -1.0 && PyErr_Occurred()) throw Refused{};
+    const double scale = PyFloat_AsDouble(a[9]), cap = PyFloat_AsDouble(a[19]);
+    if ((scale == -1.0 || cap == -1.0) && PyErr_Occurred()) throw Refused{};
+    const smetric_scores scores{float(cap), array<const float>(d, a[20], at::kFloat, "slopes")};
+    if (a[20] != Py_None && THPVariable_Unpack(a[20]).numel() != n_q)
+      refuse(PyExc_ValueError, "%s: expected one per query head", "slopes");
     const int32_t max_new = whole32(a[10]), window = whole32(a[11]);
     const void *plan = address<const void>(a[12]);
     void *workspace = address<void>(a[14]);
@@ -277,14 +296,14 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int32_t *status = array<int32_t>(d, a[16], at::kInt, "status");
     const hipStream_t s = stream(d);
     return unlocked([&] {
-      return smetric_attend(code_of(type), cache, &batch, n_q, &q, &out, lse, float(scale), max_new, window, plan, plan_bytes,
-                            workspace, ws_bytes, status, s);
+      return smetric_attend_scores(code_of(type), cache, &batch, n_q, &q, &out, lse, float(scale), &scores, max_new, window,
+                                   plan, plan_bytes, workspace, ws_bytes, status, s);
     });
   });
 }
 
 #define CALL(f) #f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
-PyMethodDef methods[] = {{CALL(qk_rotate)}, {CALL(append)}, {CALL(make_plan)}, {CALL(attend)}, {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {{CALL(qk_rotate)}, {CALL(append)}, {CALL(read)}, {CALL(make_plan)}, {CALL(attend)}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

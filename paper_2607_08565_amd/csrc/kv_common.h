@@ -21,11 +21,19 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr int32_t MAX_PLACES = 1 << 24;  // cached tokens of a request
 constexpr float E4M3_MAX = 448.0f;
+constexpr int GROUP4 = 32;  // components of E2M1 pages with one exponent
+
+// What pages hold: the activations' 16 bits, E4M3 or E2M1.
+enum Pages { PAGES16 = 0, PAGES8 = 1, PAGES4 = 2 };
+constexpr int page_bytes(Pages p, int components) {
+  return p == PAGES16 ? 2 * components : p == PAGES8 ? components : components / 2;
+}
 
 // Activation types: one struct per type with what the kernels ask of it.
 struct Bf16 {
   typedef bf16x8 V8;
   static constexpr uint32_t EXP = 0x7F807F80u, ONE_EXP = 0x00800080u;  // exponent bits, their lowest (both halves)
+  static constexpr uint32_t EXP4_MIN = 127 - 125, EXP4_MAX = 127 + 125;  // exponents whose E2M1 values it holds exactly
   // weights are held times a power of two, for few rows and for many (whose maximum may lag by 2^8)
   static constexpr float FEW_SHIFT = 0.0f, MANY_SHIFT = 0.0f;
   __device__ static __forceinline__ float lo(uint32_t x) { return __uint_as_float(x << 16); }
@@ -38,6 +46,16 @@ struct Bf16 {
   __device__ static __forceinline__ uint32_t from_e4m3(uint32_t x) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, HIGH));
   }
+  // Two of the eight E2M1 values in x, times scale, a power of two given as a float (its exponent
+  // is what is read; all ones: NaN), rounded to nearest: checked for every byte and exponent.
+  template <int PAIR>
+  __device__ static __forceinline__ uint32_t from_e2m1(uint32_t x, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, PAIR));
+  }
+  // eight of them
+  __device__ static __forceinline__ u32x4 eight_e2m1(uint32_t x, float scale) {
+    return u32x4{from_e2m1<0>(x, scale), from_e2m1<1>(x, scale), from_e2m1<2>(x, scale), from_e2m1<3>(x, scale)};
+  }
   __device__ static __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
   }
@@ -48,6 +66,7 @@ struct Bf16 {
 struct F16 {
   typedef f16x8 V8;
   static constexpr uint32_t EXP = 0x7C007C00u, ONE_EXP = 0x04000400u;
+  static constexpr uint32_t EXP4_MIN = 127 - 23, EXP4_MAX = 127 + 13;
   // as large as the type allows (2^15), for it holds weights below 2^-14 with fewer than 11 bits
   static constexpr float FEW_SHIFT = 15.0f, MANY_SHIFT = 7.0f;
   __device__ static __forceinline__ float lo(uint32_t x) { return float(__builtin_bit_cast(f16x2, x).x); }
@@ -59,6 +78,14 @@ struct F16 {
   __device__ static __forceinline__ uint32_t from_e4m3(uint32_t x) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, HIGH));
   }
+  template <int PAIR>
+  __device__ static __forceinline__ uint32_t from_e2m1(uint32_t x, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, scale, PAIR));
+  }
+  // eight of them
+  __device__ static __forceinline__ u32x4 eight_e2m1(uint32_t x, float scale) {
+    return u32x4{from_e2m1<0>(x, scale), from_e2m1<1>(x, scale), from_e2m1<2>(x, scale), from_e2m1<3>(x, scale)};
+  }
   __device__ static __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
   }
@@ -66,6 +93,17 @@ struct F16 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
   }
 };
+
+// An exponent byte as the power of two that it stands for (255: all exponent bits, NaN to from_e2m1;
+// 0: zero's bits, which from_e2m1 takes for 2^-127).
+__device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e << 23); }
+
+// Orders a wavefront's LDS accesses; no instruction.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 __device__ __forceinline__ void set_status(int32_t *status, int err) {
   if (status) atomicCAS(status, 0, err);
@@ -88,6 +126,7 @@ struct PageSide {
 };
 struct CacheView {
   PageSide k, v;
+  PageSide k_exp, v_exp;  // E2M1 pages' exponents
   const float *k_scale, *v_scale;
   const int32_t *table;
   int64_t table_stride;
@@ -99,6 +138,25 @@ struct HeadsView {  // strides in elements of 16 bits
   int64_t token, head;
 };
 
+// Request of token t: the last r with q_off[r] <= t.  64 lanes bisect together (two rounds
+// of one load up to 4,096 requests instead of a chain of twelve) for the wavefront's first
+// token; its other tokens are a few steps on.
+__device__ __forceinline__ int32_t request_of(const int64_t *__restrict__ q_off, int32_t n_req, int64_t first, int64_t t,
+                                              int lane) {
+  int32_t lo = 0, hi = n_req;  // the answer is in [lo, hi), if anywhere
+  while (hi - lo > 1) {
+    const int32_t step = (hi - lo + 63) / 64;
+    const int32_t at = lo + lane * step;
+    const bool le = at < hi && q_off[at] <= first;
+    const int n = __popcll(__ballot(le));
+    if (n == 0) break;
+    lo += (n - 1) * step;
+    hi = lo + step < hi ? lo + step : hi;
+  }
+  while (lo + 1 < n_req && q_off[lo + 1] <= t) ++lo;
+  return lo;
+}
+
 // Host checks shared by the entry points (defined with the append).
 bool heads_ok(const smetric_heads *h);
 bool cache_ok(const smetric_kv_cache *c, int32_t dtype);
@@ -106,6 +164,9 @@ bool batch_ok(const smetric_batch *b);
 CacheView cache_view(const smetric_kv_cache *c, const smetric_batch *b);
 inline HeadsView heads_view(const smetric_heads *h) {
   return h ? HeadsView{static_cast<uint16_t *>(h->data), h->token_stride, h->head_stride} : HeadsView{nullptr, 0, 0};
+}
+inline Pages pages_of(const smetric_kv_cache *c) {
+  return c->dtype == SMETRIC_E4M3 ? PAGES8 : c->dtype == SMETRIC_E2M1 ? PAGES4 : PAGES16;
 }
 inline int hip_status(hipError_t e) { return e == hipSuccess ? SMETRIC_OK : SMETRIC_EHIP; }
 

@@ -28,11 +28,6 @@ namespace {
 constexpr int FW = 4;     // wavefronts
 constexpr int FK = 32;    // keys of a wavefront's block
 
-__device__ __forceinline__ void wave_fence() {  // orders the wavefront's LDS accesses; no instruction
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 // Over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float max4(float x) {
   const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
@@ -48,13 +43,16 @@ __device__ __forceinline__ float sum4(float x) {
 }
 
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
-template <typename T, bool KV8, int D, bool WIDE>
+// SCORES: they are capped or have a bias by distance.
+template <typename T, Pages KV, int D, bool WIDE, bool SCORES>
 __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) {
-  constexpr int ESZ = KV8 ? 1 : 2;
+  constexpr bool KV8 = KV == PAGES8, KV4 = KV == PAGES4;
+  constexpr int PB = KV4 ? piece4(D) : 16;    // bytes of a lane's load
+  constexpr int ROW = page_bytes(KV, D);      // bytes of a row in memory
   constexpr int STEPS = D / 32;               // matrix steps over the components
-  constexpr int KL = D * ESZ / 64;            // 16-byte loads of a lane for 16 keys
-  constexpr int VL = FK * D * ESZ / 1024;     // 16-byte loads of a lane for a block's values
-  constexpr int VROW = D * ESZ / 16;          // lanes per row of values
+  constexpr int KL = ROW / (4 * PB);          // loads of a lane for 16 keys
+  constexpr int VL = FK * ROW / (64 * PB);    // loads of a lane for a block's values
+  constexpr int VROW = ROW / PB;              // lanes per row of values
   constexpr int VRPI = 64 / VROW;             // rows per load
   constexpr int DT = D / 16;
   constexpr int PADDED = D + 4;               // floats of a row in the joining of the wavefronts
@@ -99,7 +97,9 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
     u32x4 q[STEPS];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      const int d = KV8 ? (s / 2) * 64 + grp * 16 + (s % 2) * 8 : s * 32 + grp * 8;
+      // the components that the lane's pieces of keys hold, in their order
+      constexpr int PER = PB * 8 / (KV4 ? 4 : KV8 ? 8 : 16) / 8;  // steps of a piece
+      const int d = (s / PER) * (32 * PER) + grp * (8 * PER) + (s % PER) * 8;
       q[s] = u32x4{0, 0, 0, 0};
       if (has_row)
         q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + d);
@@ -108,67 +108,75 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
     const char *vbase = a.cache.v.base + kvh * a.cache.v.head;
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
     const float sc = a.scale_log2 * (KV8 && a.cache.k_scale ? a.cache.k_scale[kvh] : 1.0f);
+    const Capped capped(a, sc);
+    const float slope = SCORES && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
     char *my = lds + wave * REGION;
 
     const int32_t kb0 = k0 / KEY_STEP * KEY_STEP + FK * wave;
     const int32_t last_key = k1 - 1;
     u32x4 kr[2][KL], vr[VL];
+    uint32_t kx[2][KL], vx[VL];  // E2M1: their exponents
     bool bad_page = false;
-    // Where a place's keys and values are; a page outside the cache reads page 0.
-    const auto find = [&](int32_t key, uint64_t &kp, uint64_t &vp) {
-      const int32_t page = page_of(a.cache.ps, key);
-      int32_t id = table[page];
-      if (uint32_t(id) >= uint32_t(a.cache.n_pages)) {
-        id = 0;
-        bad_page = true;
-      }
-      const int32_t slot = key - page * a.cache.ps.size;
-      kp = reinterpret_cast<uint64_t>(kbase) + id * a.cache.k.page + slot * a.cache.k.token;
-      vp = reinterpret_cast<uint64_t>(vbase) + id * a.cache.v.page + slot * a.cache.v.token;
-    };
+    const auto find = [&](int32_t key, Place &p) { bad_page |= find_place<KV>(a, table, kvh, key, p); };
     // WIDE: lane l knows where the 16 keys l % 2 of the wavefront's block l / 2 from known_from
     // on are
-    uint64_t kp_l = 0, vp_l = 0;
+    Place at_l{};
     int32_t known_from = 0;
     const auto find_blocks = [&](int32_t kb) {
       int32_t key = kb + (lane >> 1) * (FK * FW) + (lane & 1) * 16;
       key = key < last_key ? key : last_key;  // 16 keys outside [k0, k1) read a neighbour's places: in bounds, not seen
       key = key > k0 ? key : k0;
-      find(key & ~15, kp_l, vp_l);
+      find(key & ~15, at_l);
       known_from = kb;
     };
+    // in E2M1 a group's exponent is that of the piece it lies in, or of the two pieces
+    const auto group = [](int piece) { return D == 64 ? piece / 2 : piece; };
     const auto load_block = [&](int32_t kb) {
       if (WIDE) {
         const int from = (kb - known_from) / (FK * FW) * 2;
-        const uint32_t ko = uint32_t(col) * uint32_t(a.cache.k.token) + grp * 16;
-        const uint32_t vo = uint32_t(lane / VROW) * uint32_t(a.cache.v.token) + (lane % VROW) * 16;
+        const uint32_t ko = uint32_t(col) * uint32_t(a.cache.k.token) + grp * PB;
+        const uint32_t vo = uint32_t(lane / VROW) * uint32_t(a.cache.v.token) + (lane % VROW) * PB;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const char *kp = reinterpret_cast<const char *>(read_lane(kp_l, from + j));
-          const char *vp = reinterpret_cast<const char *>(read_lane(vp_l, from + j));
+          const uint64_t kp = read_lane(at_l.k, from + j), vp = read_lane(at_l.v, from + j);
 #pragma unroll
-          for (int s = 0; s < KL; ++s) kr[j][s] = *reinterpret_cast<const u32x4 *>(kp + ko + s * 64);
+          for (int s = 0; s < KL; ++s) kr[j][s] = load_piece<PB>(kp + ko + s * (4 * PB));
 #pragma unroll
           for (int i = 0; i < VL / 2; ++i)
-            vr[j * (VL / 2) + i] =
-                *reinterpret_cast<const u32x4 *>(vp + vo + uint32_t(i * VRPI) * uint32_t(a.cache.v.token));
+            vr[j * (VL / 2) + i] = load_piece<PB>(vp + vo + uint32_t(i * VRPI) * uint32_t(a.cache.v.token));
+          if (KV4) {
+            const uint64_t ke = read_lane(at_l.k_exp, from + j), ve = read_lane(at_l.v_exp, from + j);
+#pragma unroll
+            for (int s = 0; s < KL; ++s)
+              kx[j][s] = load_exp(ke + (uint32_t(col) * uint32_t(a.cache.k_exp.token) + group(grp + 4 * s)));
+#pragma unroll
+            for (int i = 0; i < VL / 2; ++i)
+              vx[j * (VL / 2) + i] =
+                  load_exp(ve + (uint32_t(i * VRPI + lane / VROW) * uint32_t(a.cache.v_exp.token) + group(lane % VROW)));
+          }
         }
       } else {
         int32_t key = kb + (lane & 31);
         key = key < last_key ? key : last_key;
         key = key > k0 ? key : k0;
-        uint64_t kp, vp;
-        find(key, kp, vp);
+        Place at;
+        find(key, at);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const char *p = reinterpret_cast<const char *>(__shfl(kp, 16 * j + col)) + grp * 16;
+          const uint64_t p = __shfl(at.k, 16 * j + col) + grp * PB;
 #pragma unroll
-          for (int s = 0; s < KL; ++s) kr[j][s] = *reinterpret_cast<const u32x4 *>(p + s * 64);
+          for (int s = 0; s < KL; ++s) kr[j][s] = load_piece<PB>(p + s * (4 * PB));
+          if (KV4) {
+            const uint64_t e = __shfl(at.k_exp, 16 * j + col);
+#pragma unroll
+            for (int s = 0; s < KL; ++s) kx[j][s] = load_exp(e + group(grp + 4 * s));
+          }
         }
 #pragma unroll
-        for (int i = 0; i < VL; ++i)
-          vr[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(__shfl(vp, i * VRPI + lane / VROW)) +
-                                                   (lane % VROW) * 16);
+        for (int i = 0; i < VL; ++i) {
+          vr[i] = load_piece<PB>(__shfl(at.v, i * VRPI + lane / VROW) + (lane % VROW) * PB);
+          if (KV4) vx[i] = load_exp(__shfl(at.v_exp, i * VRPI + lane / VROW) + group(lane % VROW));
+        }
       }
     };
 
@@ -195,6 +203,9 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
             const uint32_t x = t % 2 ? w.z : w.x, y = t % 2 ? w.w : w.y;
             k = u32x4{T::template from_e4m3<false>(x), T::template from_e4m3<true>(x), T::template from_e4m3<false>(y),
                       T::template from_e4m3<true>(y)};
+          } else if (KV4) {
+            constexpr int PER = PB / 4;  // steps of a piece
+            k = T::eight_e2m1(kr[j][t / PER][t % PER], power_of(kx[j][t / PER]));
           } else {
             k = kr[j][t];
           }
@@ -217,7 +228,8 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
       for (int i = 0; i < VL; ++i) {
         const int r = i * VRPI + lane / VROW, c = lane % VROW;
         u32x4 v = vr[i];
-        if (partial && (kb + r < k0 || kb + r >= k1)) v = u32x4{0, 0, 0, 0};
+        const bool outside = partial && (kb + r < k0 || kb + r >= k1);
+        if (outside) v = u32x4{0, 0, 0, 0};
         if (KV8) {
           const u32x4 x{T::template from_e4m3<false>(v.x), T::template from_e4m3<true>(v.x),
                         T::template from_e4m3<false>(v.y), T::template from_e4m3<true>(v.y)};
@@ -225,6 +237,12 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
                         T::template from_e4m3<false>(v.w), T::template from_e4m3<true>(v.w)};
           *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((2 * c) ^ (2 * (r & SWZ))) * 16)) = finite(x);
           *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((2 * c + 1) ^ (2 * (r & SWZ))) * 16)) = finite(y);
+        } else if (KV4) {
+          constexpr int N = PB / 4;
+          const float e = power_of(outside ? 127 : vx[i]);  // (its exponent may be NaN's, and 0 times that)
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+            *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((N * c + n) ^ (2 * (r & SWZ))) * 16)) = finite(T::eight_e2m1(v[n], e));
         } else {
           *reinterpret_cast<u32x4 *>(my + r * (2 * D) + ((c ^ (2 * (r & SWZ))) * 16)) = finite(v);
         }
@@ -238,7 +256,19 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
       // weights
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = s[e / 4][e % 4] * sc;
+      for (int e = 0; e < 8; ++e) p[e] = s[e / 4][e % 4];
+      if (SCORES && capped.cap > 0.0f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = capped(p[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] *= sc;
+      }
+      if (SCORES && a.slopes) {
+        const float from = slope * float(kb + 4 * grp - place);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] += fmaf(slope, float(16 * (e / 4) + e % 4), from);
+      }
       if (masked) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -279,12 +309,12 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
         if (kb >= max_lo && kb + FK <= min_hi) continue;
 #pragma unroll 1
         for (int32_t key = max(kb, k0); key < min(kb + FK, k1); ++key) {
-          uint64_t kp, vp;
-          find(key, kp, vp);
+          Place at;
+          find(key, at);
           const bool seen = key < hi && key >= lo;
 #pragma unroll
           for (int i = 0; i < DT; ++i) {
-            const f32x4 v = four_values<T, KV8>(vp, 16 * i + 4 * grp);
+            const f32x4 v = four_values<T, KV>(at, 16 * i + 4 * grp);
 #pragma unroll
             for (int k = 0; k < 4; ++k) o[i][k] = seen && !is_finite(v[k]) ? o[i][k] + v[k] : o[i][k];
           }
@@ -345,27 +375,42 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
   }
 }
 
-template <typename T, bool KV8, int D>
+#ifdef SCORED
+constexpr bool OTHER_SCORES = true;
+#else
+constexpr bool OTHER_SCORES = false;
+#endif
+template <typename T, Pages KV, int D>
 int launch_d(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
   const dim3 grid(uint32_t(max_groups * a.n_kv)), block(64 * FW);
   if (a.cache.ps.size % 16 == 0)
-    few_kernel<T, KV8, D, true><<<grid, block, 0, stream>>>(a);
+    few_kernel<T, KV, D, true, OTHER_SCORES><<<grid, block, 0, stream>>>(a);
   else
-    few_kernel<T, KV8, D, false><<<grid, block, 0, stream>>>(a);
+    few_kernel<T, KV, D, false, OTHER_SCORES><<<grid, block, 0, stream>>>(a);
   return hip_status(hipGetLastError());
 }
-template <typename T, bool KV8>
+template <typename T, Pages KV>
 int launch_k(const AttendArgs &a, int32_t d, int64_t max_groups, hipStream_t stream) {
-  return d == 64 ? launch_d<T, KV8, 64>(a, max_groups, stream)
-                 : d == 128 ? launch_d<T, KV8, 128>(a, max_groups, stream) : launch_d<T, KV8, 256>(a, max_groups, stream);
+  return d == 64 ? launch_d<T, KV, 64>(a, max_groups, stream)
+                 : d == 128 ? launch_d<T, KV, 128>(a, max_groups, stream) : launch_d<T, KV, 256>(a, max_groups, stream);
+}
+template <typename T>
+int launch_t(const AttendArgs &a, Pages p, int32_t d, int64_t max_groups, hipStream_t stream) {
+  return p == PAGES4   ? launch_k<T, PAGES4>(a, d, max_groups, stream)
+         : p == PAGES8 ? launch_k<T, PAGES8>(a, d, max_groups, stream)
+                       : launch_k<T, PAGES16>(a, d, max_groups, stream);
 }
 
 }  // namespace
 
-int launch_few(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
-  if (dtype == SMETRIC_BF16)
-    return kv8 ? launch_k<Bf16, true>(a, head_dim, max_groups, stream) : launch_k<Bf16, false>(a, head_dim, max_groups, stream);
-  return kv8 ? launch_k<F16, true>(a, head_dim, max_groups, stream) : launch_k<F16, false>(a, head_dim, max_groups, stream);
+#ifdef SCORED
+int launch_few_scores(
+#else
+int launch_few(
+#endif
+    const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
+  return dtype == SMETRIC_BF16 ? launch_t<Bf16>(a, pages, head_dim, max_groups, stream)
+                               : launch_t<F16>(a, pages, head_dim, max_groups, stream);
 }
 
 }  // namespace smk

@@ -1,0 +1,3 @@
+// The kernels of kv_few.hip with scores that are capped or have a bias by distance, compiled apart.
+#define SCORED
+#include "kv_few.hip"

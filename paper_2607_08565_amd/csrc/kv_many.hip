@@ -108,6 +108,7 @@ struct Rows {
   f32x16 o[D / 32];  // O^T: components 32 i + 8 (r / 4) + 4 half + r % 4
   float m, l;        // of the half's keys (l), of all (m)
   int32_t hi, lo;    // the keys [lo, hi) that the row sees
+  float slope;       // other scores: the bias of a key's distance, in powers of two
 };
 
 // The values of 16 keys of a step, V^T as the matrix instruction takes it: read in the order in
@@ -134,10 +135,11 @@ struct Values {
 
 // One step's 64 keys: the scores.  S^T: lane (half, col) gets row col's scores of keys kb +
 // 32 j + 8 (r / 4) + 4 half + r % 4, -inf for those that the row does not see (MASKED: there
-// may be some).  Returns the row's largest, and the first 16 keys' values on their way.
-template <typename T, int D, bool MASKED>
-__device__ __forceinline__ float scores(const Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc, int lane,
-                                        f32x16 (&s)[2], Values<D> &first) {
+// may be some).  Returns the row's largest, and the first 16 keys' values on their way.  SCORES:
+// capped or with a bias by distance, in powers of two already.
+template <typename T, int D, bool MASKED, bool SCORES>
+__device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, const char *kl, const char *vl, int32_t kb,
+                                        float sc, int lane, f32x16 (&s)[2], Values<D> &first) {
   constexpr int N = D / 8, AHEAD = 4, ROWB = 2 * D;
   const int l = again(lane), col = l & 31, swap = 16 * ((l >> 5) ^ key_swap<D>(col));
   const char *row = kl + col * ROWB;
@@ -161,6 +163,28 @@ __device__ __forceinline__ float scores(const Rows<D> &w, const char *kl, const 
   in_order();
   __builtin_amdgcn_s_setprio(0);
   first.read(vl, Values<D>::offset(again(lane)), 0);
+  if (SCORES) {
+    if (a.cap_log2 > 0.0f) {
+      const Capped capped(a, sc);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[j][r] = capped(s[j][r]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[j][r] *= sc;
+    }
+    if (a.slopes) {
+      const float from = w.slope * float(kb + 4 * (lane >> 5) - (w.hi - 1));
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[j][r] += fmaf(w.slope, float(32 * j + 8 * (r / 4) + r % 4), from);
+    }
+    sc = 1.0f;
+  }
   if (MASKED) {
     const int half = lane >> 5;
     const int32_t hi = w.hi - kb - 4 * half, lo = w.lo - kb - 4 * half;
@@ -251,11 +275,12 @@ __device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown
 }
 
 // A step.  ENDS: not every row sees all of its keys.
-template <typename T, int D, bool ENDS>
-__device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc, int lane) {
+template <typename T, int D, bool ENDS, bool SCORES>
+__device__ __forceinline__ void step(const AttendArgs &a, Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc,
+                                     int lane) {
   f32x16 s[2];
   Values<D> first;
-  const float mx = scores<T, D, ENDS>(w, kl, vl, kb, sc, lane, s, first);
+  const float mx = scores<T, D, ENDS, SCORES>(a, w, kl, vl, kb, sc, lane, s, first);
   const uint64_t grown = __ballot(mx > w.m + SLACK);  // also the first time: m is -inf
   float down = 1.0f;
   if (grown) {  // only the rows that have grown: another one's scores change nothing in a row
@@ -266,7 +291,7 @@ __device__ __forceinline__ void step(Rows<D> &w, const char *kl, const char *vl,
   }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
-  products<T>(w, vl, sc, lane, s, first);
+  products<T>(w, vl, SCORES ? 1.0f : sc, lane, s, first);
 }
 
 // A wavefront's rows: the output, or the sums for the joining.
@@ -310,8 +335,8 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
 // What a row sees of a value that is not finite, added to what write_rows has written.  Weights
 // are positive: infinities and NaN come through as they are.  A lane takes the components that it
 // has written.  Rare, and here, where the sums' registers are free, at no cost to the steps.
-template <typename T, bool KV8, int D>
-__device__ __forceinline__ void add_not_finite(const AttendArgs &a, const PlanItem &it, uint64_t value, int32_t kvh, int wave,
+template <typename T, Pages KV, int D>
+__device__ __forceinline__ void add_not_finite(const AttendArgs &a, const PlanItem &it, const Place &place, int32_t kvh, int wave,
                                                int lane, float vs) {
   const int col = lane & 31, half = lane >> 5;
   const int32_t row = it.tile * MANY_ROWS + 32 * wave + col, tok = row / a.group, head = kvh * a.group + row % a.group;
@@ -319,7 +344,7 @@ __device__ __forceinline__ void add_not_finite(const AttendArgs &a, const PlanIt
 #pragma unroll 1
   for (int n = 0; n < D / 8; ++n) {
     const int c = it.part < 0 ? 16 * (n / 2) + 8 * half + 4 * (n % 2) : 8 * n + 4 * half;
-    const f32x4 v = four_values<T, KV8>(value, c);
+    const f32x4 v = four_values<T, KV>(place, c);
     if (is_finite(v[0]) && is_finite(v[1]) && is_finite(v[2]) && is_finite(v[3])) continue;
     u32x2 *out = reinterpret_cast<u32x2 *>(a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head + c);
     f32x4 *sum = reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + c);
@@ -335,10 +360,11 @@ __device__ __forceinline__ void add_not_finite(const AttendArgs &a, const PlanIt
 }
 
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
-template <typename T, bool KV8, int D, bool WIDE>
+template <typename T, Pages KV, int D, bool WIDE, bool SCORES>
 __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
-  constexpr int ESZ = KV8 ? 1 : 2;
-  constexpr int LPR = D * ESZ / 16;   // lanes per row of keys or values
+  constexpr bool KV8 = KV == PAGES8, KV4 = KV == PAGES4;
+  constexpr int PB = KV4 ? piece4(D) : 16;  // bytes of a lane's load
+  constexpr int LPR = page_bytes(KV, D) / PB;  // lanes per row of keys or values
   constexpr int RPW = 64 / LPR;       // rows of a wavefront's load
   constexpr int RPL = RPW * MW;       // rows of a workgroup's load
   constexpr int NL = KT / RPL;        // loads of a lane per step and side
@@ -375,6 +401,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     const int32_t first = it.kv_len - it.n_new;  // the first new token's place
     w.hi = has_row ? first + tok + 1 : 0;
     w.lo = a.window > 0 ? first + tok + 1 - a.window : 0;
+    w.slope = SCORES && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
     // the wavefront's first and last row, and the tile's
     const int32_t min_hi = first + row0 / a.group + 1;
     const int32_t max_hi = n_rows > 0 ? first + (row0 + n_rows - 1) / a.group + 1 : 0;
@@ -411,34 +438,22 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
       for (int r = 0; r < 16; ++r) w.o[i][r] = 0.0f;
     w.m = -INFINITY;
     w.l = 0.0f;
-    const char *kbase = a.cache.k.base + kvh * a.cache.k.head;
-    const char *vbase = a.cache.v.base + kvh * a.cache.v.head;
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
 
     const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
-    u32x4 kr[KV8 ? NL : 1], vr[KV8 ? NL : 1];  // 8-bit keys and values on their way to LDS
+    u32x4 kr[KV == PAGES16 ? 1 : NL], vr[KV == PAGES16 ? 1 : NL];  // 8- and 4-bit keys and values on their way to LDS
+    uint32_t kx[KV4 ? NL : 1], vx[KV4 ? NL : 1];                   // the exponents of 4-bit ones
     const int lrow = lane / LPR, lcol = lane % LPR;
     bool bad_page = false;
-    // Where a place's keys and values are; a page outside the cache reads page 0.
-    const auto find = [&](int32_t key, uint64_t &kp, uint64_t &vp) {
-      const int32_t page = page_of(a.cache.ps, key);
-      int32_t id = table[page];
-      if (uint32_t(id) >= uint32_t(a.cache.n_pages)) {
-        id = 0;
-        bad_page = true;
-      }
-      const int32_t slot = key - page * a.cache.ps.size;
-      kp = reinterpret_cast<uint64_t>(kbase) + id * a.cache.k.page + slot * a.cache.k.token;
-      vp = reinterpret_cast<uint64_t>(vbase) + id * a.cache.v.page + slot * a.cache.v.token;
-    };
+    const auto find = [&](int32_t key, Place &p) { bad_page |= find_place<KV>(a, table, kvh, key, p); };
     // WIDE: lane l knows where the 16 keys from known_from + 16 l on are, for 16 steps at a time
-    uint64_t kp_l = 0, vp_l = 0;
+    Place at_l{};
     int32_t known_from = 0;
     const auto find_steps = [&](int32_t kb) {
       int32_t key = kb + 16 * lane;  // 16 keys outside [k0, k1) read a neighbour's places: in bounds, not seen
       key = key < last_key ? key : last_key;
       key = key > k0 ? key : k0;
-      find(key & ~15, kp_l, vp_l);
+      find(key & ~15, at_l);
       known_from = kb;
     };
     const uint32_t k_lane = uint32_t(lrow) * uint32_t(a.cache.k.token), v_lane = uint32_t(lrow) * uint32_t(a.cache.v.token);
@@ -449,24 +464,37 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int r = i * RPL + wave * RPW;  // the wavefront's first row
-        const int kc = KV8 ? lcol : lcol ^ key_swap<D>(r + lrow), vc = KV8 ? lcol : lcol ^ value_swap<D>(r + lrow);
+        const int kc = KV != PAGES16 ? lcol : lcol ^ key_swap<D>(r + lrow);
+        const int vc = KV != PAGES16 ? lcol : lcol ^ value_swap<D>(r + lrow);
         uint64_t kp, vp;
-        uint32_t ko = kc * 16, vo = vc * 16;
+        uint32_t ko = kc * PB, vo = vc * PB;
         if (WIDE) {
           const int from = (kb - known_from + r) / 16;
-          kp = read_lane(kp_l, from);
-          vp = read_lane(vp_l, from);
+          kp = read_lane(at_l.k, from);
+          vp = read_lane(at_l.v, from);
+          if (KV4) {
+            const uint32_t row = r % 16 + lrow, g = D == 64 ? lcol / 2 : lcol;
+            kx[i] = load_exp(read_lane(at_l.k_exp, from) + (row * uint32_t(a.cache.k_exp.token) + g));
+            vx[i] = load_exp(read_lane(at_l.v_exp, from) + (row * uint32_t(a.cache.v_exp.token) + g));
+          }
           ko += k_lane + uint32_t(r % 16) * uint32_t(a.cache.k.token);
           vo += v_lane + uint32_t(r % 16) * uint32_t(a.cache.v.token);
         } else {
           int32_t key = kb + r + lrow;
           key = key < last_key ? key : last_key;
           key = key > k0 ? key : k0;
-          find(key, kp, vp);
+          Place at;
+          find(key, at);
+          kp = at.k;
+          vp = at.v;
+          if (KV4) {
+            kx[i] = load_exp(at.k_exp + (D == 64 ? lcol / 2 : lcol));
+            vx[i] = load_exp(at.v_exp + (D == 64 ? lcol / 2 : lcol));
+          }
         }
-        if (KV8) {
-          kr[i] = *reinterpret_cast<const u32x4 *>(kp + ko);
-          vr[i] = *reinterpret_cast<const u32x4 *>(vp + vo);
+        if (KV != PAGES16) {
+          kr[i] = load_piece<PB>(kp + ko);
+          vr[i] = load_piece<PB>(vp + vo);
         } else if (WIDE) {
           to_lds(kp, ko, kl + r * ROWB, vp, vo, vl + r * ROWB);
         } else {
@@ -479,6 +507,16 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int r = i * RPL + wave * RPW + lrow;
+        if (KV4) {
+          constexpr int N = PB / 4;
+          const float ke = power_of(kx[i]), ve = power_of(vx[i]);
+#pragma unroll
+          for (int n = 0; n < N; ++n) {
+            *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((N * lcol + n) ^ key_swap<D>(r)) * 16) = T::eight_e2m1(kr[i][n], ke);
+            *reinterpret_cast<u32x4 *>(vl + r * ROWB + ((N * lcol + n) ^ value_swap<D>(r)) * 16) = T::eight_e2m1(vr[i][n], ve);
+          }
+          continue;
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const u32x4 k = kr[i], v = vr[i];
@@ -535,8 +573,8 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
         load_next(kb);
         if (ENDS) look_over(kb, here() + SIDE);
         if (!ENDS || (n_rows > 0 && kb < max_hi && kb + KT > min_lo))
-          step<T, D, ENDS>(w, here(), here() + SIDE, kb, sc, lane);
-        if (KV8 && kb + KT < k1) to_16(there());
+          step<T, D, ENDS, SCORES>(a, w, here(), here() + SIDE, kb, sc, lane);
+        if (KV != PAGES16 && kb + KT < k1) to_16(there());
         arrived();
       }
     };
@@ -546,7 +584,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     if (kb0 < k1) {
       if (WIDE) find_steps(kb0);
       load_step(kb0, here());
-      if (KV8) to_16(here());
+      if (KV != PAGES16) to_16(here());
       arrived();
       int32_t kb = kb0;
 #pragma unroll 1
@@ -567,35 +605,50 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
       for (int32_t key = k0; key < k1; ++key) {
         if (key >= full0 && key < full1) key = full1;
         if (key >= k1) break;
-        uint64_t kp, vp;
-        find(key, kp, vp);
-        if (key < w.hi && key >= w.lo) add_not_finite<T, KV8, D>(a, it, vp, kvh, wave, lane, vs);
+        Place at;
+        find(key, at);
+        if (key < w.hi && key >= w.lo) add_not_finite<T, KV, D>(a, it, at, kvh, wave, lane, vs);
       }
     }
   }
 }
 
-template <typename T, bool KV8, int D>
+#ifdef SCORED
+constexpr bool OTHER_SCORES = true;
+#else
+constexpr bool OTHER_SCORES = false;
+#endif
+template <typename T, Pages KV, int D>
 int launch_d(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
   const dim3 grid(uint32_t(max_groups * a.n_kv)), block(MT);
   if (a.cache.ps.size % 16 == 0)
-    many_kernel<T, KV8, D, true><<<grid, block, 0, stream>>>(a);
+    many_kernel<T, KV, D, true, OTHER_SCORES><<<grid, block, 0, stream>>>(a);
   else
-    many_kernel<T, KV8, D, false><<<grid, block, 0, stream>>>(a);
+    many_kernel<T, KV, D, false, OTHER_SCORES><<<grid, block, 0, stream>>>(a);
   return hip_status(hipGetLastError());
 }
-template <typename T, bool KV8>
+template <typename T, Pages KV>
 int launch_k(const AttendArgs &a, int32_t d, int64_t max_groups, hipStream_t stream) {
-  return d == 64 ? launch_d<T, KV8, 64>(a, max_groups, stream)
-                 : d == 128 ? launch_d<T, KV8, 128>(a, max_groups, stream) : launch_d<T, KV8, 256>(a, max_groups, stream);
+  return d == 64 ? launch_d<T, KV, 64>(a, max_groups, stream)
+                 : d == 128 ? launch_d<T, KV, 128>(a, max_groups, stream) : launch_d<T, KV, 256>(a, max_groups, stream);
+}
+template <typename T>
+int launch_t(const AttendArgs &a, Pages p, int32_t d, int64_t max_groups, hipStream_t stream) {
+  return p == PAGES4   ? launch_k<T, PAGES4>(a, d, max_groups, stream)
+         : p == PAGES8 ? launch_k<T, PAGES8>(a, d, max_groups, stream)
+                       : launch_k<T, PAGES16>(a, d, max_groups, stream);
 }
 
 }  // namespace
 
-int launch_many(const AttendArgs &a, int32_t dtype, bool kv8, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
-  if (dtype == SMETRIC_BF16)
-    return kv8 ? launch_k<Bf16, true>(a, head_dim, max_groups, stream) : launch_k<Bf16, false>(a, head_dim, max_groups, stream);
-  return kv8 ? launch_k<F16, true>(a, head_dim, max_groups, stream) : launch_k<F16, false>(a, head_dim, max_groups, stream);
+#ifdef SCORED
+int launch_many_scores(
+#else
+int launch_many(
+#endif
+    const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
+  return dtype == SMETRIC_BF16 ? launch_t<Bf16>(a, pages, head_dim, max_groups, stream)
+                               : launch_t<F16>(a, pages, head_dim, max_groups, stream);
 }
 
 }  // namespace smk

@@ -317,6 +317,9 @@ int launch_join(const AttendArgs &a, int32_t head_dim, int64_t max_splits, hipSt
 // A window of all places is none: what the kernels subtract from a place stays in 32 bits.
 int32_t window_of(int32_t window) { return window >= MAX_PLACES ? 0 : window; }
 
+// Caps whose rates and products stay far from float32's ends.
+constexpr float CAP_MIN = 0x1p-20f, CAP_MAX = 0x1p20f;
+
 bool shape_ok(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t max_new) {
   return n_req >= 0 && n_tokens >= 0 && (n_req > 0 || n_tokens == 0) && n_kv >= 1 && n_q >= n_kv && n_q <= 65536 &&
          n_q % n_kv == 0 && n_tokens * (n_q / n_kv) < 0x7FFFFFFF && n_tokens <= 0x7FFFFFFF && max_new >= 1 &&
@@ -356,10 +359,14 @@ extern "C" int smetric_attend_plan(const int64_t *q_off, const int32_t *kv_len, 
   return hip_status(hipGetLastError());
 }
 
-extern "C" int smetric_attend(int32_t dtype, const smetric_kv_cache *cache, const smetric_batch *batch, int32_t n_q_heads,
-                              const smetric_heads *q, const smetric_heads *out, float *lse, float scale, int32_t max_new,
-                              int32_t window, const void *plan, uint64_t plan_bytes, void *workspace, uint64_t ws_bytes,
-                              int32_t *status, hipStream_t stream) {
+extern "C" int smetric_attend_scores(int32_t dtype, const smetric_kv_cache *cache, const smetric_batch *batch,
+                                     int32_t n_q_heads, const smetric_heads *q, const smetric_heads *out, float *lse,
+                                     float scale, const smetric_scores *scores, int32_t max_new, int32_t window,
+                                     const void *plan, uint64_t plan_bytes, void *workspace, uint64_t ws_bytes,
+                                     int32_t *status, hipStream_t stream) {
+  if (!scores || !(scores->cap == 0.0f || (scores->cap >= CAP_MIN && scores->cap <= CAP_MAX)) ||
+      reinterpret_cast<uintptr_t>(scores->slopes) % 4)
+    return SMETRIC_EINVAL;
   if (!cache_ok(cache, dtype) || !batch_ok(batch) || window < 0 || !(scale > 0.0f) || !isfinite(scale) ||
       !shape_ok(batch->n_req, batch->n_tokens, n_q_heads, cache->n_kv_heads, cache->head_dim, max_new))
     return SMETRIC_EINVAL;
@@ -392,12 +399,24 @@ extern "C" int smetric_attend(int32_t dtype, const smetric_kv_cache *cache, cons
   a.rows = s.rows;
   a.dim = cache->head_dim;
   a.window = window_of(window);
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = scale * LOG2E;
+  a.cap_log2 = scores->cap * LOG2E;
+  a.slopes = scores->slopes;
   a.status = status;
-  const bool kv8 = cache->dtype == SMETRIC_E4M3;
-  int rc = s.rows == FEW_ROWS ? launch_few(a, dtype, kv8, cache->head_dim, s.max_groups, stream)
-                              : launch_many(a, dtype, kv8, cache->head_dim, s.max_groups, stream);
+  const bool few = s.rows == FEW_ROWS;
+  const auto launch = scores->cap > 0.0f || scores->slopes ? few ? launch_few_scores : launch_many_scores
+                                                           : few ? launch_few : launch_many;
+  const int rc = launch(a, dtype, pages_of(cache), cache->head_dim, s.max_groups, stream);
   if (rc != SMETRIC_OK) return rc;
   return dtype == SMETRIC_BF16 ? launch_join<Bf16>(a, cache->head_dim, s.max_splits, stream)
                                : launch_join<F16>(a, cache->head_dim, s.max_splits, stream);
+}
+
+extern "C" int smetric_attend(int32_t dtype, const smetric_kv_cache *cache, const smetric_batch *batch, int32_t n_q_heads,
+                              const smetric_heads *q, const smetric_heads *out, float *lse, float scale, int32_t max_new,
+                              int32_t window, const void *plan, uint64_t plan_bytes, void *workspace, uint64_t ws_bytes,
+                              int32_t *status, hipStream_t stream) {
+  const smetric_scores plain{0.0f, nullptr};
+  return smetric_attend_scores(dtype, cache, batch, n_q_heads, q, out, lse, scale, &plain, max_new, window, plan, plan_bytes,
+                               workspace, ws_bytes, status, stream);
 }

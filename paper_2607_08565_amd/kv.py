@@ -7,7 +7,7 @@ model's layer on a batch of requests, each with one new token or a chunk of them
     q = kv.append(cache, table, q_off, kv_len, k, v, q=q, rotary=rotary)  # per layer
     out = kv.attend(q, cache, table, plan)
 
-Tensors go in by data pointer on torch's current stream of the current device, which has to be
+and, for an instance that hands a request's tokens on, kv.read of what the pages hold.  Tensors go in by data pointer on torch's current stream of the current device, which has to be
 theirs; there is no CPU fallback.
 """
 from __future__ import annotations
@@ -23,13 +23,20 @@ try:
 except ImportError as e:
     raise RuntimeError("_kv_calls.so is missing or does not fit: build it first (__graft_entry__.build())") from e
 
-_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
+_E2M1, _E8M0 = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu  # two components a byte; a group's exponent
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2, _E2M1: 3}
+GROUP = 32  # components of a 4-bit cache with one exponent
+
+
+class _Exps(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3)]
 
 
 class _Cache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("k_stride", C.c_int64 * 3),
                 ("v_stride", C.c_int64 * 3), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
-                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("exps", C.c_void_p)]
 
 
 class _Rotary(C.Structure):
@@ -51,14 +58,17 @@ def _device(*tensors: torch.Tensor | None) -> int:
 
 class PagedCache:
     """Keys and values in pages: two tensors [n_pages, n_kv_heads, page_size, head_dim] of any
-    strides with contiguous components (a view of another order is one), bfloat16, float16
-    or float8_e4m3fn -- then with float32 scales per head: a stored x stands for x * scale."""
+    strides with contiguous components (a view of another order is one), bfloat16, float16,
+    float8_e4m3fn -- then with float32 scales per head: a stored x stands for x * scale -- or
+    float4_e2m1fn_x2, whose last dimension is head_dim / 2 bytes of two components, with exponents
+    k_exp and v_exp, float8_e8m0fnu [n_pages, n_kv_heads, page_size, head_dim / 32]: a stored x
+    stands for x * 2^(e - 127)."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
-                 v_scale: torch.Tensor | None = None):
+                 v_scale: torch.Tensor | None = None, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None):
         for t, name in ((k, "k"), (v, "v")):
             if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or t.dim() != 4:
-                raise TypeError(f"{name}: expected a CUDA tensor [pages, heads, page_size, head_dim] of 16 or 8 bits")
+                raise TypeError(f"{name}: expected a CUDA tensor [pages, heads, page_size, head_dim] of 16, 8 or 4 bits")
             if t.stride(3) != 1:
                 raise ValueError(f"{name}: components must be contiguous")
         if k.shape != v.shape or k.dtype != v.dtype:
@@ -68,20 +78,38 @@ class PagedCache:
         if k_scale is not None and (k.dtype != torch.float8_e4m3fn or k_scale.numel() != k.shape[1] or
                                     v_scale.numel() != k.shape[1]):
             raise ValueError("scales: one per head of a float8_e4m3fn cache")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        per = 2 if k.dtype == _E2M1 else 1  # components of an element of the tensor
+        exps = ((k_exp, "k_exp"), (v_exp, "v_exp"))
+        for t, name in exps:
+            if (t is None) == (per == 2):
+                raise ValueError("k_exp and v_exp: both with a float4_e2m1fn_x2 cache, neither with another one")
+            if t is not None and (not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != _E8M0):
+                raise TypeError(f"{name}: expected a float8_e8m0fnu CUDA tensor")
+            if t is not None and (t.shape != (*k.shape[:3], 2 * k.shape[3] // GROUP) or t.stride(3) != 1):
+                raise ValueError(f"{name}: expected one per {GROUP} components, those of a token contiguous")
+        self.k, self.v, self.k_scale, self.v_scale, self.k_exp, self.v_exp = k, v, k_scale, v_scale, k_exp, v_exp
+        self.n_pages, self.n_kv_heads, self.page_size = k.shape[:3]
+        self.head_dim = per * k.shape[3]
         self.dtype = k.dtype
-        self.c = _Cache(k.data_ptr(), v.data_ptr(), self.n_pages, (C.c_int64 * 3)(*k.stride()[:3]),
-                        (C.c_int64 * 3)(*v.stride()[:3]), self.page_size, self.n_kv_heads, self.head_dim,
-                        _DTYPES[k.dtype], _opt(k_scale, torch.float32, "k_scale"),
+        strides = lambda t, n: (C.c_int64 * 3)(*[n * x for x in t.stride()[:3]])  # noqa: E731
+        self.c = _Cache(k.data_ptr(), v.data_ptr(), self.n_pages, strides(k, per), strides(v, per), self.page_size,
+                        self.n_kv_heads, self.head_dim, _DTYPES[k.dtype], _opt(k_scale, torch.float32, "k_scale"),
                         _opt(v_scale, torch.float32, "v_scale"))
-        self.device = _device(k, v, k_scale, v_scale)
+        if per == 2:
+            self.exps = _Exps(k_exp.data_ptr(), v_exp.data_ptr(), strides(k_exp, 1), strides(v_exp, 1))
+            self.c.exps = C.addressof(self.exps)
+        self.device = _device(k, v, k_scale, v_scale, k_exp, v_exp)
         self.ref = C.addressof(self.c)
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 16,
               dtype: torch.dtype = torch.bfloat16, device="cuda", **scales) -> "PagedCache":
         shape = (n_pages, n_kv_heads, page_size, head_dim)
+        if dtype == _E2M1:
+            # a page's two exponents of a head beside each other: at heads of 128 and pages of 16 one line of memory
+            e = torch.empty((n_pages, n_kv_heads, 2, page_size, head_dim // GROUP), dtype=_E8M0, device=device)
+            shape = (*shape[:3], head_dim // 2)
+            scales = dict(scales, k_exp=e[:, :, 0], v_exp=e[:, :, 1])
         return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device), **scales)
 
 
@@ -137,6 +165,28 @@ def append(cache: PagedCache, page_table: torch.Tensor, q_off: torch.Tensor, kv_
     return q_out if q is not None else None
 
 
+def read(cache: PagedCache, page_table: torch.Tensor, q_off: torch.Tensor, kv_len: torch.Tensor,
+         n_tokens: int | None = None, dtype: torch.dtype | None = None, k_out: torch.Tensor | None = None,
+         v_out: torch.Tensor | None = None, status: torch.Tensor | None = None):
+    """smetric_kv_read: the last q_off[r+1] - q_off[r] of request r's kv_len[r] cached tokens read
+    back as activations, n_tokens = q_off[-1] of all requests.  Returns (k_out, v_out)
+    [n_tokens, heads, head_dim], made of `dtype` (a 16-bit cache's own, else bfloat16) where not
+    given; n_tokens and dtype are not needed beside one that is."""
+    given = k_out if k_out is not None else v_out
+    if given is None and n_tokens is None:
+        raise ValueError("n_tokens: expected with no output given")
+    if given is None or k_out is None or v_out is None:
+        if dtype is None:
+            dtype = given.dtype if given is not None else cache.dtype if cache.dtype.itemsize == 2 else torch.bfloat16
+        n = given.shape[0] if given is not None else n_tokens
+        make = lambda: torch.empty((n, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=cache.k.device)  # noqa: E731
+        k_out, v_out = make() if k_out is None else k_out, make() if v_out is None else v_out
+    rc = _kv_calls.read(cache.ref, page_table, q_off, kv_len, k_out, v_out, status, cache.device)
+    if rc:
+        raise SmetricError("smetric_kv_read", rc)
+    return k_out, v_out
+
+
 class Plan:
     """How a step's attention is split over the GPU: made once per step from the lengths, used
     by every layer.  The buffers (plan and workspace) are kept; a plan serves any batch of the
@@ -175,10 +225,13 @@ class Plan:
 
 
 def attend(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, plan: Plan, scale: float | None = None,
-           out: torch.Tensor | None = None, lse: torch.Tensor | None = None, status: torch.Tensor | None = None):
+           out: torch.Tensor | None = None, lse: torch.Tensor | None = None, status: torch.Tensor | None = None,
+           cap: float = 0.0, slopes: torch.Tensor | None = None):
     """smetric_attend: the new tokens' attention over the pages, as `plan` (made for the batch)
     splits it.  scale: 1 / sqrt(head_dim) by default; lse (float32 [tokens, heads]) is
-    filled if given.  Returns out [tokens, heads, head_dim]."""
+    filled if given.  cap: scores become cap * tanh(score / cap); slopes (float32 [heads]): they get a
+    bias slopes[head] * (key's place - token's place) (smetric_attend_scores).  Returns out
+    [tokens, heads, head_dim]."""
     if plan.kv_len is None:
         raise ValueError("plan: make() it for the batch first")
     _, T, Hq, H, D, max_new = plan.args
@@ -187,7 +240,7 @@ def attend(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, plan: P
     out = _new(q, "q") if out is None else out
     rc = _kv_calls.attend(q, out, lse, cache.ref, page_table, plan.q_off, plan.kv_len, T, Hq,
                           D ** -0.5 if scale is None else scale, max_new, plan.window, plan.plan_ptr, plan.plan_bytes,
-                          plan.ws_ptr, plan.ws_bytes, status, cache.device, plan.device)
+                          plan.ws_ptr, plan.ws_bytes, status, cache.device, plan.device, cap, slopes)
     if rc:
-        raise SmetricError("smetric_attend", rc)
+        raise SmetricError("smetric_attend" if cap == 0 and slopes is None else "smetric_attend_scores", rc)
     return out

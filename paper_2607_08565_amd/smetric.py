@@ -92,6 +92,8 @@ def _load() -> C.CDLL:
         "smetric_kv_append": [I32, P, P, P, P, I32, P, P, P, P, P, P],
         "smetric_attend_plan_bytes": [I32, I64, I32, I32, I32, I32, P, P],
         "smetric_attend_plan": [P, P, I32, I64, I32, I32, I32, I32, I32, P, U64, P, P],
+        "smetric_kv_read": [I32, P, P, P, P, P, P],
+        "smetric_attend_scores": [I32, P, P, I32, P, P, P, C.c_float, P, I32, I32, P, U64, P, U64, P, P],
         "smetric_attend": [I32, P, P, I32, P, P, P, C.c_float, I32, I32, P, U64, P, U64, P, P],
     }
     for name, args in sig.items():
@@ -114,6 +116,7 @@ EXPORTED = (
     "smetric_route_seq_coloc_ws_bytes", "smetric_route_seq_noalloc", "smetric_route_seq_noalloc_max_req",
     "smetric_probe_stats", "smetric_route_score",
     "smetric_qk_rotate", "smetric_kv_append", "smetric_attend_plan_bytes", "smetric_attend_plan", "smetric_attend",
+    "smetric_kv_read", "smetric_attend_scores",
 )
 
 
