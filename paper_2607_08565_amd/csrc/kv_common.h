@@ -138,24 +138,55 @@ struct HeadsView {  // strides in elements of 16 bits
   int64_t token, head;
 };
 
-// Request of token t: the last r with q_off[r] <= t.  64 lanes bisect together (two rounds
-// of one load up to 4,096 requests instead of a chain of twelve) for the wavefront's first
-// token; its other tokens are a few steps on.
-__device__ __forceinline__ int32_t request_of(const int64_t *__restrict__ q_off, int32_t n_req, int64_t first, int64_t t,
-                                              int lane) {
-  int32_t lo = 0, hi = n_req;  // the answer is in [lo, hi), if anywhere
-  while (hi - lo > 1) {
-    const int32_t step = (hi - lo + 63) / 64;
-    const int32_t at = lo + lane * step;
-    const bool le = at < hi && q_off[at] <= first;
-    const int n = __popcll(__ballot(le));
-    if (n == 0) break;
-    lo += (n - 1) * step;
-    hi = lo + step < hi ? lo + step : hi;
+// The request of a token t, the last r with q_off[r] <= t, and its numbers.
+struct Request {
+  int32_t r, len;    // kv_len
+  int64_t from, to;  // its tokens
+};
+// Where a wavefront finds its tokens' requests: 64 of them from that of its first token on, each lane
+// holding one's numbers, so that they come from memory in one round instead of a chain of loads.
+// All lanes make it and ask it together.
+struct Requests {
+  const int64_t *q_off;
+  const int32_t *kv_len;
+  int32_t n_req, lo, len;
+  int64_t from, to;
+  // first: the first token, the same for all lanes.  They bisect until 64 requests are left: no
+  // round up to 64 requests, one up to 4,096.
+  __device__ __forceinline__ Requests(const int64_t *__restrict__ off, const int32_t *__restrict__ lens, int32_t n,
+                                      int64_t first, int lane)
+      : q_off(off), kv_len(lens), n_req(n), lo(0) {
+    int32_t hi = n_req;  // the answer is in [lo, hi), if anywhere
+    while (hi - lo > 64) {
+      const int32_t step = (hi - lo + 63) / 64;
+      const int32_t at = lo + lane * step;
+      const int k = __popcll(__ballot(at < hi && q_off[at] <= first));
+      if (k == 0) break;
+      lo += (k - 1) * step;
+      hi = lo + step < hi ? lo + step : hi;
+    }
+    const int32_t at = lo + lane < n_req ? lo + lane : n_req - 1;
+    from = q_off[at];
+    to = q_off[at + 1];
+    len = kv_len[at];
   }
-  while (lo + 1 < n_req && q_off[lo + 1] <= t) ++lo;
-  return lo;
-}
+  // In order: t is at least what the lane asked for before, `in` where that was found (0 at first).
+  __device__ __forceinline__ Request of(int64_t t, int &in) const {
+    int64_t z = __shfl(to, in);
+    for (;;) {
+      const bool on = z <= t && in < 63 && lo + in + 1 < n_req;
+      if (!__any(on)) break;
+      in += on;
+      z = __shfl(to, in);
+    }
+    Request q{lo + in, __shfl(len, in), __shfl(from, in), z};
+    if (z <= t && q.r + 1 < n_req) {  // past the 64
+      while (q.r + 1 < n_req && q_off[q.r + 1] <= t) ++q.r;
+      q = Request{q.r, kv_len[q.r], q_off[q.r], q_off[q.r + 1]};
+    }
+    return q;
+  }
+};
 
 // Host checks shared by the entry points (defined with the append).
 bool heads_ok(const smetric_heads *h);

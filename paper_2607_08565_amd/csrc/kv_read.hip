@@ -9,7 +9,7 @@ namespace smk {
 namespace {
 
 constexpr int ET = 256;  // threads per workgroup
-constexpr int EU = 4;    // tokens of a thread
+constexpr int EU = 2;    // tokens of a thread
 
 struct ReadArgs {
   const int64_t *q_off;
@@ -36,23 +36,28 @@ __device__ __forceinline__ u32x4 widened(u32x4 x, uint32_t e, float scale) {
   return y;
 }
 
+// A workgroup takes EU tokens side by side, or several times as many: threads are dealt to (which of
+// them, head, piece), a thread's EU tokens follow each other.  blockIdx.y: 256 pieces of rows longer
+// than that.
 template <typename T, Pages KV, int D>
 __global__ __launch_bounds__(ET) void read_kernel(ReadArgs a) {
   constexpr int PPR = D / 8;  // pieces of a row
   constexpr int PB = page_bytes(KV, 8);
-  const int32_t per_block = a.n_kv * PPR;  // threads of EU tokens
-  const int64_t id = int64_t(blockIdx.x) * ET + threadIdx.x, first = (int64_t(blockIdx.x) * ET + (threadIdx.x & ~63)) / per_block * EU;
-  const int64_t t0 = id / per_block * EU;
+  const uint32_t per_token = uint32_t(a.n_kv) * PPR, side = per_token < ET ? ET / per_token : 1;
+  const int lane = threadIdx.x & 63;
+  const uint32_t which = per_token < ET ? threadIdx.x / per_token : 0;
+  const uint32_t in = per_token < ET ? threadIdx.x % per_token : blockIdx.y * ET + threadIdx.x;
+  const int64_t base = int64_t(blockIdx.x) * side * EU, t0 = base + which * EU;
+  const int64_t first = base + (per_token < ET ? (threadIdx.x & ~63u) / per_token : 0) * EU;
   if (first >= a.n_tokens) return;  // the whole wavefront
-  const int32_t in = int32_t(id % per_block), head = in / PPR, piece = in % PPR, lane = threadIdx.x & 63;
-  const bool live = t0 < a.n_tokens;
-  int32_t r = request_of(a.q_off, a.n_req, first, live ? t0 : a.n_tokens - 1, lane);
+  const bool live = t0 < a.n_tokens && which < side && in < per_token;
+  const int32_t head = in / PPR, piece = in % PPR;
+  const Requests requests(a.q_off, a.kv_len, a.n_req, first, lane);
+  int at_request = 0;
+  Request of[EU];
+#pragma unroll
+  for (int u = 0; u < EU; ++u) of[u] = requests.of(live ? (t0 + u < a.n_tokens ? t0 + u : a.n_tokens - 1) : first, at_request);
   if (!live) return;
-  float scale[2] = {1.0f, 1.0f};
-  if (KV == PAGES8 && a.cache.k_scale) {
-    scale[0] = a.cache.k_scale[head];
-    scale[1] = a.cache.v_scale[head];
-  }
   u32x4 x[EU][2];
   uint32_t e[EU][2];
   bool bad = false;
@@ -62,17 +67,15 @@ __global__ __launch_bounds__(ET) void read_kernel(ReadArgs a) {
     x[u][0] = x[u][1] = u32x4{0, 0, 0, 0};
     e[u][0] = e[u][1] = 127;
     if (t >= a.n_tokens) continue;
-    while (r + 1 < a.n_req && a.q_off[r + 1] <= t) ++r;
-    const int64_t from = a.q_off[r], to = a.q_off[r + 1];
-    const int32_t len = a.kv_len[r];
-    const int64_t p = int64_t(len) - (to - t);
-    bool ok = t >= from && t < to && len >= 0 && len <= MAX_PLACES && int64_t(len) <= int64_t(a.cache.max_pages) * a.cache.ps.size;
+    const Request &q = of[u];
+    const int64_t p = int64_t(q.len) - (q.to - t);
+    const bool ok = t >= q.from && t < q.to && q.len >= 0 && q.len <= MAX_PLACES &&
+                    int64_t(q.len) <= int64_t(a.cache.max_pages) * a.cache.ps.size;
     bad |= !ok;
-    ok = ok && p >= 0;
-    if (!ok) continue;
+    if (!ok || p < 0) continue;
     const int32_t place = int32_t(p), page = page_of(a.cache.ps, place);
-    const int32_t id4 = a.cache.table[r * a.cache.table_stride + page], slot = place - page * a.cache.ps.size;
-    if (uint32_t(id4) >= uint32_t(a.cache.n_pages)) {
+    const int32_t id = a.cache.table[q.r * a.cache.table_stride + page], slot = place - page * a.cache.ps.size;
+    if (uint32_t(id) >= uint32_t(a.cache.n_pages)) {
       bad = true;
       continue;
     }
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(ET) void read_kernel(ReadArgs a) {
     for (int s = 0; s < 2; ++s) {
       if (!a.out[s].data) continue;
       const PageSide &side = s ? a.cache.v : a.cache.k, &es = s ? a.cache.v_exp : a.cache.k_exp;
-      const char *at = side.base + id4 * side.page + head * side.head + slot * side.token + piece * PB;
+      const char *at = side.base + id * side.page + head * side.head + slot * side.token + piece * PB;
       if (KV == PAGES16) x[u][s] = *reinterpret_cast<const u32x4 *>(at);
       if (KV == PAGES8) {
         const u32x2 y = *reinterpret_cast<const u32x2 *>(at);
@@ -89,28 +92,36 @@ __global__ __launch_bounds__(ET) void read_kernel(ReadArgs a) {
       }
       if (KV == PAGES4) {
         x[u][s].x = *reinterpret_cast<const uint32_t *>(at);
-        e[u][s] = uint8_t(es.base[id4 * es.page + head * es.head + slot * es.token + piece / 4]);
+        e[u][s] = uint8_t(es.base[id * es.page + head * es.head + slot * es.token + piece / 4]);
       }
     }
   }
   if (bad) set_status(a.status, SMETRIC_EINVAL);
+  float scale[2] = {1.0f, 1.0f};
+  if (KV == PAGES8 && a.cache.k_scale) {
+    scale[0] = a.cache.k_scale[head];
+    scale[1] = a.cache.v_scale[head];
+  }
 #pragma unroll
   for (int u = 0; u < EU; ++u) {
     const int64_t t = t0 + u;
     if (t >= a.n_tokens) break;
 #pragma unroll
     for (int s = 0; s < 2; ++s)
-      if (a.out[s].data)
-        *reinterpret_cast<u32x4 *>(a.out[s].data + t * a.out[s].token + head * a.out[s].head + 8 * piece) =
-            widened<T, KV>(x[u][s], e[u][s], scale[s]);
+      if (a.out[s].data) {
+        u32x4 *to = reinterpret_cast<u32x4 *>(a.out[s].data + t * a.out[s].token + head * a.out[s].head + 8 * piece);
+        // past the caches: what is read back is more than they hold
+        __builtin_nontemporal_store(widened<T, KV>(x[u][s], e[u][s], scale[s]), to);
+      }
   }
 }
 
 template <typename T, Pages KV, int D>
 int launch_d(const ReadArgs &a, hipStream_t stream) {
-  const int64_t threads = (a.n_tokens + EU - 1) / EU * a.n_kv * (D / 8), grid = (threads + ET - 1) / ET;
-  if (grid > 0x7FFFFFFF) return SMETRIC_EINVAL;
-  read_kernel<T, KV, D><<<dim3(uint32_t(grid)), dim3(ET), 0, stream>>>(a);
+  const int64_t per_token = int64_t(a.n_kv) * (D / 8), side = per_token < ET ? ET / per_token : 1;
+  const int64_t grid = (a.n_tokens + side * EU - 1) / (side * EU), wide = per_token < ET ? 1 : (per_token + ET - 1) / ET;
+  if (grid > 0x7FFFFFFF || wide > 65535) return SMETRIC_EINVAL;
+  read_kernel<T, KV, D><<<dim3(uint32_t(grid), uint32_t(wide)), dim3(ET), 0, stream>>>(a);
   return hip_status(hipGetLastError());
 }
 template <typename T, Pages KV>

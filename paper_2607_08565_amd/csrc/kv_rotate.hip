@@ -12,9 +12,11 @@
 // order, so a wavefront reads consecutive heads of one token in one run and the token's
 // cosines and sines come from memory once and from the nearest cache for its other heads.
 //
-// Measured: 8,191 tokens of 40 heads of 128 32.1 us, 5.3 TB/s (a copy of 4 GiB moves 4.8); the
-// keys, values and queries of 6,249 tokens appended 38.1 us, 4.1 TB/s (pages in any order, the
-// queries kept in the caches for the attention); a token's append 4.4 us, its launch; of 256 5.3.
+// Measured: 8,191 tokens of 40 heads of 128 29.5 us, 5.8 TB/s (a copy of 4 GiB moves 4.8); the
+// keys, values and queries of 6,249 tokens appended 32.4 us, 4.8 TB/s (pages in any order, the
+// queries kept in the caches for the attention); keys and values of 8 heads alone into 4-bit pages
+// 13 to 14 us, where instructions and the chain to the pages are what is left (32 MB are 7 us); a
+// token's append 4.4 us, its launch; of 256 5.2.
 #include "common.h"
 #include "kv_common.h"
 
@@ -97,25 +99,43 @@ __device__ __forceinline__ uint32_t exponent_of(uint32_t bits) {
   return k < T::EXP4_MIN ? T::EXP4_MIN : k > T::EXP4_MAX ? T::EXP4_MAX : k;
 }
 
-// PAGED: k goes to the cache (places from the batch) and v exists; else k goes to k_out and
-// positions are given.
+// Rows (token, head) in order, a workgroup a run of them.  Which token one is of: divisions by the
+// heads of a token, as products with rounded-up inverses (exact for the numbers at hand: rows x heads
+// below 2^64; at most 2 RT / 4 rows past a token's first x fewer than 64 heads below 2^16).
+struct Rows {
+  uint64_t inverse;   // 2^64 / per_token, 0: one
+  uint32_t small;     // 2^16 / per_token
+  int32_t per_token;
+};
+inline Rows rows_of(int32_t per_token) {
+  return {per_token == 1 ? 0 : ~uint64_t(0) / uint32_t(per_token) + 1, 65536 / uint32_t(per_token) + 1, per_token};
+}
+
+// PAGED: k goes to the cache (places from the batch), and with it the same token's and head's v, whose
+// place is the same; else k goes to k_out and positions are given.  (E4M3: v in a row of its own, as
+// 32 divisions of a lane cost more than finding a place twice: 256 tokens 5.7 us, apart 5.2.)
+constexpr int sides_of(Pages p) { return p == PAGES8 ? 1 : 2; }  // of a row
 template <typename T, int D, bool INTER, bool PAGED, Pages KV>
 __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, CacheView cache, HeadsView q, HeadsView q_out,
                                                   HeadsView k, HeadsView k_out, HeadsView v, int64_t n_tokens, int32_t n_q,
-                                                  int32_t n_kv) {
+                                                  Rows rows) {
+  constexpr bool KV4 = KV == PAGES4;
   constexpr int LPR = D / 16;  // lanes per row
-  constexpr bool KV8 = KV == PAGES8, KV4 = KV == PAGES4;
-  const int32_t per_token = n_q + (PAGED ? 2 : 1) * n_kv;
-  const int64_t row = (int64_t(blockIdx.x) * RT + threadIdx.x) / LPR;
+  constexpr int WG = RT / LPR;  // rows of a workgroup
   const int lane = threadIdx.x & 63, sub = threadIdx.x % LPR;
-  const int64_t n_rows = n_tokens * per_token;
-  // rows of one workgroup: at most RT / LPR, so 32 bits hold the distance from its first
-  const int64_t t0 = (int64_t(blockIdx.x) * RT + (threadIdx.x & ~63)) / LPR / per_token;
-  const bool live = row < n_rows;
-  const int64_t t = live ? row / per_token : n_tokens - 1;
-  const int32_t h = live ? int32_t(row - t * per_token) : 0;
-  const int kind = h < n_q ? 0 : h < n_q + n_kv ? 1 : 2;
-  const int32_t head = kind == 0 ? h : kind == 1 ? h - n_q : h - n_q - n_kv;
+  const uint64_t row0 = uint64_t(blockIdx.x) * WG;
+  const int64_t token0 = rows.inverse ? __umul64hi(row0, rows.inverse) : row0;
+  const uint32_t in0 = uint32_t(row0 - token0 * rows.per_token);
+  const auto token_of = [&](uint32_t x) { return rows.per_token >= WG ? uint32_t(x >= uint32_t(rows.per_token)) : x * rows.small >> 16; };
+  const uint32_t x0 = in0 + threadIdx.x / LPR, dt = token_of(x0);
+  const bool live = token0 + dt < n_tokens;
+  const int64_t t = live ? token0 + dt : n_tokens - 1;
+  const int32_t h = live ? int32_t(x0 - dt * rows.per_token) : 0;
+  const bool cached = h >= n_q;  // a key (and, PAGED, a value)
+  constexpr int SIDES = PAGED ? sides_of(KV) : 1;
+  const int32_t n_kv = SIDES == 2 ? rows.per_token - n_q : (rows.per_token - n_q) / 2;
+  const bool value = PAGED && SIDES == 1 && h >= n_q + n_kv;
+  const int32_t head = h - (value ? n_q + n_kv : cached ? n_q : 0);
 
   // this lane's two pieces of 8 components
   const int half = ta.rot / 16;
@@ -125,46 +145,44 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
     c1 = sub < half ? sub + half : 2 * sub + 1;
   }
   // (which of the two turn: both or none for halves)
-  const bool turns0 = c0 < (INTER ? 2 * half : half) && kind != 2;
-  const bool turns1 = INTER ? c1 < 2 * half && kind != 2 : turns0;
+  const bool turns0 = c0 < (INTER ? 2 * half : half) && !value;
+  const bool turns1 = INTER ? c1 < 2 * half && !value : turns0;
   // asked for before the chain of loads that finds the place
-  const HeadsView &src = kind == 0 ? q : kind == 1 ? k : v;
-  const uint16_t *from = src.data + t * src.token + head * src.head;
-  const u32x4 in0 = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + 8 * c0));
-  const u32x4 in1 = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + 8 * c1));
+  const auto load = [&](const HeadsView &src, u32x4 (&in)[2]) {
+    const uint16_t *from = src.data + t * src.token + head * src.head;
+    in[0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + 8 * c0));
+    in[1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + 8 * c1));
+  };
+  u32x4 in[2], in_v[2]{};
+  load(value ? v : cached ? k : q, in);
+  if (SIDES == 2 && cached) load(v, in_v);
+  float scale = 1.0f;
+  if (KV == PAGES8 && cached && cache.k_scale) scale = (value ? cache.v_scale : cache.k_scale)[head];
 
-  int32_t place = 0, pos = 0;
-  int64_t page_row = 0, exp_row = 0;
+  int32_t place = 0, pos = 0, page = 0, id = 0;
   bool ok = live, bad = false;
   if (PAGED) {
-    // In a decoding step token t is request t's: asked for at once; a search of the whole
-    // wavefront where that is not so for one of its lanes.
-    int32_t r = t < ba.n_req ? int32_t(t) : ba.n_req - 1;
-    int64_t a = ba.q_off[r], z = ba.q_off[r + 1];
-    int32_t len = ba.kv_len[r];
-    if (__any(a > t || z <= t)) {
-      r = request_of(ba.q_off, ba.n_req, t0 < n_tokens ? t0 : n_tokens - 1, t, lane);
-      a = ba.q_off[r];
-      z = ba.q_off[r + 1];
-      len = ba.kv_len[r];
+    // In a decoding step, as many tokens as requests, token t is request t's: asked for at once, and a
+    // search of the whole wavefront only where that is not so for one of its lanes.
+    Request rq{0, 0, 0, 0};
+    const bool step = n_tokens == ba.n_req;
+    if (step) rq = Request{int32_t(t), ba.kv_len[t], ba.q_off[t], ba.q_off[t + 1]};
+    if (!step || __any(rq.from > t || rq.to <= t)) {
+      const int64_t first = token0 + token_of(in0 + (threadIdx.x & ~63u) / LPR);
+      int at = 0;
+      rq = Requests(ba.q_off, ba.kv_len, ba.n_req, first < n_tokens ? first : n_tokens - 1, lane).of(t, at);
     }
-    bad = t < a || t >= z || len < 0 || len > MAX_PLACES || int64_t(len) > int64_t(cache.max_pages) * cache.ps.size;
-    const int64_t p = int64_t(len) - (z - t);
+    bad = t < rq.from || t >= rq.to || rq.len < 0 || rq.len > MAX_PLACES ||
+          int64_t(rq.len) > int64_t(cache.max_pages) * cache.ps.size;
+    const int64_t p = int64_t(rq.len) - (rq.to - t);
     ok = ok && !bad && p >= 0;
     place = ok ? int32_t(p) : 0;
     pos = place;
     if (ok) {
-      const int32_t page = page_of(cache.ps, place);
-      const int32_t id = cache.table[r * cache.table_stride + page];
-      const bool fine = uint32_t(id) < uint32_t(cache.n_pages);
-      bad = !fine;
-      ok = fine;
-      const PageSide &s = kind == 2 ? cache.v : cache.k;
-      page_row = ok ? id * s.page + head * s.head + (place - page * cache.ps.size) * s.token : 0;
-      if (KV4) {
-        const PageSide &e = kind == 2 ? cache.v_exp : cache.k_exp;
-        exp_row = ok ? id * e.page + head * e.head + (place - page * cache.ps.size) * e.token : 0;
-      }
+      page = page_of(cache.ps, place);
+      id = cache.table[rq.r * cache.table_stride + page];
+      ok = uint32_t(id) < uint32_t(cache.n_pages);
+      bad = !ok;
     }
   }
   if (ta.rot > 0) {
@@ -177,22 +195,24 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
   if (live && bad && sub == 0) set_status(ta.status, SMETRIC_EINVAL);
 
   float x[16];
-  widen<T>(ok ? in0 : u32x4{0, 0, 0, 0}, x);
-  widen<T>(ok ? in1 : u32x4{0, 0, 0, 0}, x + 8);
-  const uint16_t *w = static_cast<const uint16_t *>(kind == 2 ? nullptr : ta.weight[kind]);
-  // the exchange is outside the condition: rows with and without a weight share a wavefront
-  float ss = 0.0f;
+  widen<T>(ok ? in[0] : u32x4{0, 0, 0, 0}, x);
+  widen<T>(ok ? in[1] : u32x4{0, 0, 0, 0}, x + 8);
+  if (ta.weight[0] || ta.weight[1]) {
+    const uint16_t *w = static_cast<const uint16_t *>(ta.weight[cached]);
+    // the exchange is outside the condition: rows with and without a weight share a wavefront
+    float ss = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
+    for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
-  for (int m = 1; m < LPR; m *= 2) ss += __shfl_xor(ss, m, 64);
-  if (w && ok) {  // (zeros stay zeros also where eps is 0)
-    const float rstd = 1.0f / sqrtf(ss * (1.0f / D) + ta.eps);
-    float g[16];
-    widen<T>(*reinterpret_cast<const u32x4 *>(w + 8 * c0), g);
-    widen<T>(*reinterpret_cast<const u32x4 *>(w + 8 * c1), g + 8);
+    for (int m = 1; m < LPR; m *= 2) ss += __shfl_xor(ss, m, 64);
+    if (w && ok && !value) {  // (zeros stay zeros also where eps is 0)
+      const float rstd = 1.0f / sqrtf(ss * (1.0f / D) + ta.eps);
+      float g[16];
+      widen<T>(*reinterpret_cast<const u32x4 *>(w + 8 * c0), g);
+      widen<T>(*reinterpret_cast<const u32x4 *>(w + 8 * c1), g + 8);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = x[i] * rstd * g[i];
+      for (int i = 0; i < 16; ++i) x[i] = x[i] * rstd * g[i];
+    }
   }
   if (ok && (turns0 || turns1)) {
     // angles: eight in a row for halves; four of each piece for neighbours
@@ -220,61 +240,85 @@ __global__ __launch_bounds__(RT) void turn_kernel(TurnArgs ta, BatchArgs ba, Cac
       b = yb * co[i] + ya * si[i];
     }
   }
-  // 4 bits: the lane that has a piece is not the one that has its neighbours, so their largest
-  // magnitudes, then the codes, pass through LDS, where a row is in order: a lane then writes two
-  // neighbouring pieces.  (All lanes: rows of queries share wavefronts with rows of the cache.)
-  uint32_t e0 = 0, e1 = 0;
-  u32x2 codes{0, 0};
-  if (KV4) {
-    __shared__ __attribute__((aligned(16))) uint32_t sh[RT * 2];
-    uint32_t *row_sh = sh + threadIdx.x / LPR * (D / 8);
-    row_sh[c0] = largest(x);
-    row_sh[c1] = largest(x + 8);
-    wave_fence();
-    const auto group = [&](int c) {
-      const u32x4 m = *reinterpret_cast<const u32x4 *>(row_sh + (c & ~3));
-      const uint32_t a = m[0] > m[1] ? m[0] : m[1], b = m[2] > m[3] ? m[2] : m[3];
-      return exponent_of<T>(a > b ? a : b);
-    };
-    e0 = group(c0);
-    e1 = group(c1);
-    wave_fence();
-    row_sh[c0] = narrow_e2m1(x, power_of(e0));
-    row_sh[c1] = narrow_e2m1(x + 8, power_of(e1));
-    wave_fence();
-    codes = *reinterpret_cast<const u32x2 *>(row_sh + 2 * sub);
+  if (PAGED) {
+    // Both sides' rows into their pages, side by side: neither waits for the other.  4 bits: the lane that has
+    // a piece is not the one that has its neighbours, so their largest magnitudes, then the codes,
+    // pass through LDS, where a row is in order: a lane then writes two neighbouring pieces.  All
+    // lanes come here together, also those of queries, which share wavefronts with keys.
+    if (__any(cached && live)) {
+      float y[SIDES][16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[0][i] = x[i];
+      if (SIDES == 2) {
+        widen<T>(in_v[0], y[SIDES - 1]);
+        widen<T>(in_v[1], y[SIDES - 1] + 8);
+      }
+      uint32_t e[SIDES][2];
+      u32x2 codes[SIDES][2];
+      if (KV4) {
+        __shared__ __attribute__((aligned(16))) uint32_t sh[SIDES][RT * 2];
+        const int row = threadIdx.x / LPR * (D / 8);
+#pragma unroll
+        for (int s = 0; s < SIDES; ++s) {
+          sh[s][row + c0] = largest(y[s]);
+          sh[s][row + c1] = largest(y[s] + 8);
+        }
+        wave_fence();
+#pragma unroll
+        for (int s = 0; s < SIDES; ++s)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const u32x4 m = *reinterpret_cast<const u32x4 *>(&sh[s][row + ((i ? c1 : c0) & ~3)]);
+            const uint32_t a = m[0] > m[1] ? m[0] : m[1], b = m[2] > m[3] ? m[2] : m[3];
+            e[s][i] = exponent_of<T>(a > b ? a : b);
+          }
+        wave_fence();
+#pragma unroll
+        for (int s = 0; s < SIDES; ++s) {
+          sh[s][row + c0] = narrow_e2m1(y[s], power_of(e[s][0]));
+          sh[s][row + c1] = narrow_e2m1(y[s] + 8, power_of(e[s][1]));
+        }
+        wave_fence();
+#pragma unroll
+        for (int s = 0; s < SIDES; ++s) codes[s][0] = *reinterpret_cast<const u32x2 *>(&sh[s][row + 2 * sub]);
+      } else if (KV == PAGES8) {
+#pragma unroll
+        for (int s = 0; s < SIDES; ++s)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) codes[s][i] = narrow_e4m3(y[s] + 8 * i, scale);
+      }
+      if (ok && cached) {
+        const int32_t slot = place - page * cache.ps.size;
+#pragma unroll
+        for (int s = 0; s < SIDES; ++s) {
+          const PageSide &side = s || value ? cache.v : cache.k;
+          char *to = side.base + (id * side.page + head * side.head + slot * side.token);
+          if (KV4) {
+            const PageSide &es = s ? cache.v_exp : cache.k_exp;
+            *reinterpret_cast<u32x2 *>(to + 8 * sub) = codes[s][0];
+            char *ex = es.base + (id * es.page + head * es.head + slot * es.token);
+            if (c0 % 4 == 0) ex[c0 / 4] = char(e[s][0]);
+            if (c1 % 4 == 0) ex[c1 / 4] = char(e[s][1]);
+          } else if (KV == PAGES8) {
+            *reinterpret_cast<u32x2 *>(to + 8 * c0) = codes[s][0];
+            *reinterpret_cast<u32x2 *>(to + 8 * c1) = codes[s][1];
+          } else {
+            *reinterpret_cast<u32x4 *>(to + 16 * c0) = narrow<T>(y[s]);
+            *reinterpret_cast<u32x4 *>(to + 16 * c1) = narrow<T>(y[s] + 8);
+          }
+        }
+      }
+    }
   }
-  if (!live) return;
-  if (PAGED && kind != 0) {
-    if (!ok) return;
-    if (KV4) {
-      const PageSide &s = kind == 1 ? cache.k : cache.v, &e = kind == 1 ? cache.k_exp : cache.v_exp;
-      *reinterpret_cast<u32x2 *>(s.base + page_row + 8 * sub) = codes;
-      if (c0 % 4 == 0) e.base[exp_row + c0 / 4] = char(e0);
-      if (c1 % 4 == 0) e.base[exp_row + c1 / 4] = char(e1);
-      return;
-    }
-    const PageSide &s = kind == 1 ? cache.k : cache.v;
-    char *p = s.base + page_row;
-    if (KV8) {
-      const float *sc = kind == 1 ? cache.k_scale : cache.v_scale;
-      const float scale = sc ? sc[head] : 1.0f;
-      *reinterpret_cast<u32x2 *>(p + 8 * c0) = narrow_e4m3(x, scale);
-      *reinterpret_cast<u32x2 *>(p + 8 * c1) = narrow_e4m3(x + 8, scale);
-    } else {
-      *reinterpret_cast<u32x4 *>(p + 16 * c0) = narrow<T>(x);
-      *reinterpret_cast<u32x4 *>(p + 16 * c1) = narrow<T>(x + 8);
-    }
+  if (!live || (PAGED && cached)) return;
+  const HeadsView &dst = cached ? k_out : q_out;
+  uint16_t *p = dst.data + t * dst.token + head * dst.head;
+  if (PAGED) {  // attention reads it next
+    *reinterpret_cast<u32x4 *>(p + 8 * c0) = narrow<T>(x);
+    *reinterpret_cast<u32x4 *>(p + 8 * c1) = narrow<T>(x + 8);
   } else {
-    const HeadsView &dst = kind == 0 ? q_out : k_out;
-    uint16_t *p = dst.data + t * dst.token + head * dst.head;
-    if (PAGED) {  // attention reads it next
-      *reinterpret_cast<u32x4 *>(p + 8 * c0) = narrow<T>(x);
-      *reinterpret_cast<u32x4 *>(p + 8 * c1) = narrow<T>(x + 8);
-    } else {
-      __builtin_nontemporal_store(narrow<T>(x), reinterpret_cast<u32x4 *>(p + 8 * c0));
-      __builtin_nontemporal_store(narrow<T>(x + 8), reinterpret_cast<u32x4 *>(p + 8 * c1));
-    }
+    __builtin_nontemporal_store(narrow<T>(x), reinterpret_cast<u32x4 *>(p + 8 * c0));
+    __builtin_nontemporal_store(narrow<T>(x + 8), reinterpret_cast<u32x4 *>(p + 8 * c1));
   }
 }
 
@@ -291,11 +335,11 @@ struct Launch {
 };
 template <typename T, int D, bool INTER, bool PAGED, Pages KV>
 int launch(const Launch &a) {
-  const int64_t rows = a.n_tokens * (a.n_q + int64_t(a.paged ? 2 : 1) * a.n_kv), wg = RT / (D / 16);
-  const int64_t grid = (rows + wg - 1) / wg;
+  const int32_t per_token = a.n_q + (PAGED ? 3 - sides_of(KV) : 1) * a.n_kv;
+  const int64_t wg = RT / (D / 16), grid = (a.n_tokens * per_token + wg - 1) / wg;
   if (grid > 0x7FFFFFFF) return SMETRIC_EINVAL;
   turn_kernel<T, D, INTER, PAGED, KV><<<dim3(uint32_t(grid)), dim3(RT), 0, a.stream>>>(
-      a.ta, a.ba, a.cache, a.q, a.q_out, a.k, a.k_out, a.v, a.n_tokens, a.n_q, a.n_kv);
+      a.ta, a.ba, a.cache, a.q, a.q_out, a.k, a.k_out, a.v, a.n_tokens, a.n_q, rows_of(per_token));
   return hip_status(hipGetLastError());
 }
 template <typename T, int D, bool INTER>
