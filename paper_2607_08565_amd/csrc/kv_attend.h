@@ -146,13 +146,25 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, const int32_t *t
 // What a lane takes of a row of E2M1 at once: 16 bytes, a group with one exponent; of the 32 bytes of
 // a head of 64 half a group, so that 16 rows are a wavefront's load as with the others.
 constexpr int piece4(int head_dim) { return head_dim == 64 ? 8 : 16; }
+// From an address that is known to be memory's: a load that might be LDS's counts as one of both, and
+// then every read of LDS waits for the keys and values on their way.
+template <typename V>
+__device__ __forceinline__ V from_memory(uint64_t p, uint32_t offset = 0) {
+  return *(const __attribute__((address_space(1))) V *)((const __attribute__((address_space(1))) char *)p + offset);
+}
 template <int BYTES>
-__device__ __forceinline__ u32x4 load_piece(uint64_t p) {
-  if (BYTES == 16) return *reinterpret_cast<const u32x4 *>(p);
-  const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+__device__ __forceinline__ u32x4 load_piece(uint64_t p, uint32_t offset = 0) {
+  if (BYTES == 16) return from_memory<u32x4>(p, offset);
+  const u32x2 x = from_memory<u32x2>(p, offset);
   return u32x4{x.x, x.y, 0, 0};
 }
-__device__ __forceinline__ uint32_t load_exp(uint64_t p) { return *reinterpret_cast<const uint8_t *>(p); }
+__device__ __forceinline__ uint32_t load_exp(uint64_t p, uint32_t offset = 0) { return from_memory<uint8_t>(p, offset); }
+
+// x, computed again in every step: what follows from it is not kept in registers across them.
+__device__ __forceinline__ int again(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
 // Other scores (smetric_attend_scores), in powers of two: of x = q . k, sc = scale log2(e) (and the keys'
 // scale), the capped score, cap tanh(scale x / cap) = cap - 2 cap / (1 + exp(2 scale x / cap)): both ends
@@ -190,14 +202,14 @@ template <typename T, Pages KV>
 __device__ __forceinline__ f32x4 four_values(const Place &p, int c) {
   u32x2 x;
   if (KV == PAGES4) {
-    const uint32_t y = *reinterpret_cast<const uint16_t *>(p.v + c / 2);
+    const uint32_t y = from_memory<uint16_t>(p.v + c / 2);
     const float e = power_of(load_exp(p.v_exp + c / GROUP4));
     x = u32x2{T::template from_e2m1<0>(y, e), T::template from_e2m1<1>(y, e)};
   } else if (KV == PAGES8) {
-    const uint32_t y = *reinterpret_cast<const uint32_t *>(p.v + c);
+    const uint32_t y = from_memory<uint32_t>(p.v + c);
     x = u32x2{T::template from_e4m3<false>(y), T::template from_e4m3<true>(y)};
   } else {
-    x = *reinterpret_cast<const u32x2 *>(p.v + 2 * c);
+    x = from_memory<u32x2>(p.v + 2 * c);
   }
   return f32x4{T::lo(x.x), T::hi(x.x), T::lo(x.y), T::hi(x.y)};
 }

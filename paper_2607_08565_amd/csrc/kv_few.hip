@@ -25,8 +25,13 @@
 namespace smk {
 namespace {
 
-constexpr int FW = 4;     // wavefronts
 constexpr int FK = 32;    // keys of a wavefront's block
+constexpr int NJ = FK / 16;
+// Wavefronts of a workgroup.  The next block is on its way during a block's products: of 4-bit heads of 64
+// that is 2 KB, and eight wavefronts on a compute unit keep 17 KB under way where 5.6 TB/s need some
+// 45; with twice as many 32 requests decoding over 16,384 take 70 us for 85.  (Heads of 128 and 256 need the
+// registers: with eight they spill.  Blocks of 64 keys: heads of 64 73 us, of 128 no faster, 87 for 85.)
+constexpr int few_waves(Pages p, int head_dim) { return p == PAGES4 && head_dim == 64 ? 8 : 4; }
 
 // Over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float max4(float x) {
@@ -45,8 +50,10 @@ __device__ __forceinline__ float sum4(float x) {
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
 // SCORES: they are capped or have a bias by distance.
 template <typename T, Pages KV, int D, bool WIDE, bool SCORES>
-__global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D) / 4) void few_kernel(AttendArgs a) {
+  constexpr int FW = few_waves(KV, D);        // wavefronts
   constexpr bool KV8 = KV == PAGES8, KV4 = KV == PAGES4;
+  constexpr bool LATE = KV4 && !SCORES;       // scores are multiplied by their factor, positive here, on the way to weights
   constexpr int PB = KV4 ? piece4(D) : 16;    // bytes of a lane's load
   constexpr int ROW = page_bytes(KV, D);      // bytes of a row in memory
   constexpr int STEPS = D / 32;               // matrix steps over the components
@@ -56,10 +63,10 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
   constexpr int VRPI = 64 / VROW;             // rows per load
   constexpr int DT = D / 16;
   constexpr int PADDED = D + 4;               // floats of a row in the joining of the wavefronts
-  constexpr int REGION = 16 * PADDED * 4;     // bytes of a wavefront's LDS: 32 rows of values, later its sums
+  // bytes of a wavefront's LDS: rows of values, later its sums; whole rows, as addresses are exchanged within one
+  constexpr int SUMS = (16 * PADDED * 4 + 2 * D - 1) / (2 * D) * (2 * D), REGION = FK * 2 * D > SUMS ? FK * 2 * D : SUMS;
   constexpr int SWZ = D == 64 ? 3 : 7;
-  static_assert(REGION >= FK * D * 2, "values fit");
-  __shared__ __attribute__((aligned(16))) char lds[FW * REGION];
+  __shared__ __attribute__((aligned(2 * D))) char lds[FW * REGION];
   __shared__ float ml[FW][16][2];
 
   const int32_t kvh = blockIdx.x % a.n_kv, share = blockIdx.x / a.n_kv;
@@ -104,26 +111,31 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
       if (has_row)
         q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + d);
     }
-    const char *kbase = a.cache.k.base + kvh * a.cache.k.head;
-    const char *vbase = a.cache.v.base + kvh * a.cache.v.head;
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
     const float sc = a.scale_log2 * (KV8 && a.cache.k_scale ? a.cache.k_scale[kvh] : 1.0f);
     const Capped capped(a, sc);
     const float slope = SCORES && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
     char *my = lds + wave * REGION;
+    // Where in LDS a lane's values go: 16-byte piece c of row r at c ^ 2 (r & SWZ), so that the transposed
+    // reads, of eight rows' two pieces at a time, meet no bank twice.  What depends on the lane is
+    // computed here; a load's and a piece's share is exchanged in (its bits lie within a row).
+    constexpr int PIECES = 2 * D / 16 / VROW;  // 16-byte pieces in LDS of a lane's load
+    const int r0 = lane / VROW, tr = 4 * grp + col / 4;
+    const int to = wave * REGION + r0 * (2 * D) + ((PIECES * (lane % VROW)) ^ (2 * (r0 & SWZ))) * 16;
+    const int from_t = wave * REGION + tr * (2 * D) + (((col % 4) / 2) ^ (2 * (tr & SWZ))) * 16 + (col & 1) * 8;
 
     const int32_t kb0 = k0 / KEY_STEP * KEY_STEP + FK * wave;
     const int32_t last_key = k1 - 1;
-    u32x4 kr[2][KL], vr[VL];
-    uint32_t kx[2][KL], vx[VL];  // E2M1: their exponents
+    u32x4 kr[NJ][KL], vr[VL];
+    uint32_t kx[NJ][KL], vx[VL];  // E2M1: their exponents
     bool bad_page = false;
     const auto find = [&](int32_t key, Place &p) { bad_page |= find_place<KV>(a, table, kvh, key, p); };
-    // WIDE: lane l knows where the 16 keys l % 2 of the wavefront's block l / 2 from known_from
+    // WIDE: lane l knows where the 16 keys l % NJ of the wavefront's block l / NJ from known_from
     // on are
     Place at_l{};
     int32_t known_from = 0;
     const auto find_blocks = [&](int32_t kb) {
-      int32_t key = kb + (lane >> 1) * (FK * FW) + (lane & 1) * 16;
+      int32_t key = kb + (lane / NJ) * (FK * FW) + (lane % NJ) * 16;
       key = key < last_key ? key : last_key;  // 16 keys outside [k0, k1) read a neighbour's places: in bounds, not seen
       key = key > k0 ? key : k0;
       find(key & ~15, at_l);
@@ -131,38 +143,38 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
     };
     // in E2M1 a group's exponent is that of the piece it lies in, or of the two pieces
     const auto group = [](int piece) { return D == 64 ? piece / 2 : piece; };
+    const uint32_t k_lane = uint32_t(col) * uint32_t(a.cache.k.token) + grp * PB;
+    const uint32_t v_lane = uint32_t(r0) * uint32_t(a.cache.v.token) + (lane % VROW) * PB;
+    const uint32_t ke_lane = KV4 ? uint32_t(col) * uint32_t(a.cache.k_exp.token) + group(grp) : 0;
+    const uint32_t ve_lane = KV4 ? uint32_t(r0) * uint32_t(a.cache.v_exp.token) + group(lane % VROW) : 0;
     const auto load_block = [&](int32_t kb) {
       if (WIDE) {
-        const int from = (kb - known_from) / (FK * FW) * 2;
-        const uint32_t ko = uint32_t(col) * uint32_t(a.cache.k.token) + grp * PB;
-        const uint32_t vo = uint32_t(lane / VROW) * uint32_t(a.cache.v.token) + (lane % VROW) * PB;
+        const int from = (kb - known_from) / (FK * FW) * NJ;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < NJ; ++j) {
           const uint64_t kp = read_lane(at_l.k, from + j), vp = read_lane(at_l.v, from + j);
 #pragma unroll
-          for (int s = 0; s < KL; ++s) kr[j][s] = load_piece<PB>(kp + ko + s * (4 * PB));
+          for (int s = 0; s < KL; ++s) kr[j][s] = load_piece<PB>(kp, k_lane + s * (4 * PB));
 #pragma unroll
-          for (int i = 0; i < VL / 2; ++i)
-            vr[j * (VL / 2) + i] = load_piece<PB>(vp + vo + uint32_t(i * VRPI) * uint32_t(a.cache.v.token));
+          for (int i = 0; i < VL / NJ; ++i)
+            vr[j * (VL / NJ) + i] = load_piece<PB>(vp, v_lane + uint32_t(i * VRPI) * uint32_t(a.cache.v.token));
           if (KV4) {
             const uint64_t ke = read_lane(at_l.k_exp, from + j), ve = read_lane(at_l.v_exp, from + j);
 #pragma unroll
-            for (int s = 0; s < KL; ++s)
-              kx[j][s] = load_exp(ke + (uint32_t(col) * uint32_t(a.cache.k_exp.token) + group(grp + 4 * s)));
+            for (int s = 0; s < KL; ++s) kx[j][s] = load_exp(ke, ke_lane + 4 * s);
 #pragma unroll
-            for (int i = 0; i < VL / 2; ++i)
-              vx[j * (VL / 2) + i] =
-                  load_exp(ve + (uint32_t(i * VRPI + lane / VROW) * uint32_t(a.cache.v_exp.token) + group(lane % VROW)));
+            for (int i = 0; i < VL / NJ; ++i)
+              vx[j * (VL / NJ) + i] = load_exp(ve, ve_lane + uint32_t(i * VRPI) * uint32_t(a.cache.v_exp.token));
           }
         }
       } else {
-        int32_t key = kb + (lane & 31);
+        int32_t key = kb + (lane & (FK - 1));
         key = key < last_key ? key : last_key;
         key = key > k0 ? key : k0;
         Place at;
         find(key, at);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < NJ; ++j) {
           const uint64_t p = __shfl(at.k, 16 * j + col) + grp * PB;
 #pragma unroll
           for (int s = 0; s < KL; ++s) kr[j][s] = load_piece<PB>(p + s * (4 * PB));
@@ -174,8 +186,8 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
         }
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
-          vr[i] = load_piece<PB>(__shfl(at.v, i * VRPI + lane / VROW) + (lane % VROW) * PB);
-          if (KV4) vx[i] = load_exp(__shfl(at.v_exp, i * VRPI + lane / VROW) + group(lane % VROW));
+          vr[i] = load_piece<PB>(__shfl(at.v, i * VRPI + r0) + (lane % VROW) * PB);
+          if (KV4) vx[i] = load_exp(__shfl(at.v_exp, i * VRPI + r0) + group(lane % VROW));
         }
       }
     };
@@ -191,9 +203,9 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
     }
     for (int32_t kb = kb0; kb < k1; kb += FK * FW) {
       // S^T: lane (grp, col) gets row col's scores of keys kb + 16 j + 4 grp + r
-      f32x4 s[2];
+      f32x4 s[NJ];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < NJ; ++j) {
         s[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int t = 0; t < STEPS; ++t) {
@@ -213,73 +225,77 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
         }
       }
       const bool partial = kb < k0 || kb + FK > k1, masked = kb < max_lo || kb + FK > min_hi;
-      // values to LDS, as 16-bit rows whose 16-byte pieces are exchanged within the row; zeros in
-      // place of those that are not finite where rows differ in what they see, as 0 times them must
-      // not reach a row that does not see them (added in the end, from memory again, to the rows that
-      // do: weights are positive, infinities and NaN come through as they are)
+      // Values to LDS, as 16-bit rows; zeros in place of those that are not finite where rows differ
+      // in what they see, as 0 times them must not reach a row that does not see them (added in the
+      // end, from memory again, to the rows that do: weights are positive, infinities and NaN come
+      // through as they are).
       const bool apart = masked && !one_token;
-      const auto finite = [&](u32x4 x) {
-        if (!apart || !any_not_finite<T>(x)) return x;
-        odd = true;
-        return finite_only<T>(x);
-      };
       wave_fence();
+      const int to_now = KV4 ? again(to) : to, from_now = KV4 ? again(from_t) : from_t;
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
-        const int r = i * VRPI + lane / VROW, c = lane % VROW;
-        u32x4 v = vr[i];
-        const bool outside = partial && (kb + r < k0 || kb + r >= k1);
-        if (outside) v = u32x4{0, 0, 0, 0};
-        if (KV8) {
-          const u32x4 x{T::template from_e4m3<false>(v.x), T::template from_e4m3<true>(v.x),
-                        T::template from_e4m3<false>(v.y), T::template from_e4m3<true>(v.y)};
-          const u32x4 y{T::template from_e4m3<false>(v.z), T::template from_e4m3<true>(v.z),
-                        T::template from_e4m3<false>(v.w), T::template from_e4m3<true>(v.w)};
-          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((2 * c) ^ (2 * (r & SWZ))) * 16)) = finite(x);
-          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((2 * c + 1) ^ (2 * (r & SWZ))) * 16)) = finite(y);
-        } else if (KV4) {
-          constexpr int N = PB / 4;
-          const float e = power_of(outside ? 127 : vx[i]);  // (its exponent may be NaN's, and 0 times that)
-#pragma unroll
-          for (int n = 0; n < N; ++n)
-            *reinterpret_cast<u32x4 *>(my + r * (2 * D) + (((N * c + n) ^ (2 * (r & SWZ))) * 16)) = finite(T::eight_e2m1(v[n], e));
-        } else {
-          *reinterpret_cast<u32x4 *>(my + r * (2 * D) + ((c ^ (2 * (r & SWZ))) * 16)) = finite(v);
+        u32x4 v = vr[i], w[PIECES];
+        uint32_t e = KV4 ? vx[i] : 0;
+        if (partial && (kb + i * VRPI + r0 < k0 || kb + i * VRPI + r0 >= k1)) {
+          v = u32x4{0, 0, 0, 0};
+          e = 127;  // (it may be a NaN's, and 0 times that)
         }
+        if (KV8) {
+          w[0] = u32x4{T::template from_e4m3<false>(v.x), T::template from_e4m3<true>(v.x), T::template from_e4m3<false>(v.y),
+                       T::template from_e4m3<true>(v.y)};
+          w[PIECES - 1] = u32x4{T::template from_e4m3<false>(v.z), T::template from_e4m3<true>(v.z), T::template from_e4m3<false>(v.w),
+                           T::template from_e4m3<true>(v.w)};
+        } else if (KV4) {
+#pragma unroll
+          for (int n = 0; n < PIECES; ++n) w[n] = T::eight_e2m1(v[n], power_of(e));
+        } else {
+          w[0] = v;
+        }
+        if (apart) {
+#pragma unroll
+          for (int n = 0; n < PIECES; ++n)
+            if (any_not_finite<T>(w[n])) {
+              odd = true;
+              w[n] = finite_only<T>(w[n]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < PIECES; ++n)
+          *reinterpret_cast<u32x4 *>(lds + (to_now ^ 16 * (n ^ (2 * ((i * VRPI) & SWZ)))) + i * VRPI * (2 * D)) = w[n];
       }
       wave_fence();
       const int32_t next = kb + FK * FW;
       if (next < k1) {
-        if (WIDE && next - known_from >= 32 * FK * FW) find_blocks(next);
+        if (WIDE && next - known_from >= 64 / NJ * FK * FW) find_blocks(next);
         load_block(next);
       }
       // weights
-      float p[8];
+      float p[4 * NJ];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = s[e / 4][e % 4];
+      for (int e = 0; e < 4 * NJ; ++e) p[e] = s[e / 4][e % 4];
       if (SCORES && capped.cap > 0.0f) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = capped(p[e]);
-      } else {
+        for (int e = 0; e < 4 * NJ; ++e) p[e] = capped(p[e]);
+      } else if (!LATE) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] *= sc;
+        for (int e = 0; e < 4 * NJ; ++e) p[e] *= sc;
       }
       if (SCORES && a.slopes) {
         const float from = slope * float(kb + 4 * grp - place);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] += fmaf(slope, float(16 * (e / 4) + e % 4), from);
+        for (int e = 0; e < 4 * NJ; ++e) p[e] += fmaf(slope, float(16 * (e / 4) + e % 4), from);
       }
       if (masked) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4 * NJ; ++e) {
           const int32_t key = kb + 16 * (e / 4) + 4 * grp + e % 4;
           if (key >= hi || key < lo) p[e] = -INFINITY;
         }
       }
       float mx = p[0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, p[e]);
-      mx = max4(mx);
+      for (int e = 1; e < 4 * NJ; ++e) mx = fmaxf(mx, p[e]);
+      mx = max4(LATE ? mx * sc : mx);
       if (__any(mx > m)) {
         const float mn = fmaxf(m, mx);
         const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
@@ -290,17 +306,20 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
       }
       const float base = (m == -INFINITY ? 0.0f : m) - T::FEW_SHIFT;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(p[e] - base);
+      for (int e = 0; e < 4 * NJ; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(LATE ? fmaf(p[e], sc, -base) : p[e] - base);
         l += p[e];
       }
-      const u32x4 pw{T::pack(p[0], p[1]), T::pack(p[2], p[3]), T::pack(p[4], p[5]), T::pack(p[6], p[7])};
 #pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        const int r = 4 * grp + col / 4, c = 2 * i + (col % 4) / 2;
-        const char *x = my + r * (2 * D) + ((c ^ (2 * (r & SWZ))) * 16) + (col & 1) * 8;
-        const u32x2 v0 = read_transposed(x), v1 = read_transposed(x + 16 * (2 * D));  // r + 16: the same exchange
-        o[i] = T::mfma16(u32x4{v0.x, v0.y, v1.x, v1.y}, pw, o[i]);
+      for (int t = 0; t < NJ / 2; ++t) {
+        const u32x4 pw{T::pack(p[8 * t], p[8 * t + 1]), T::pack(p[8 * t + 2], p[8 * t + 3]), T::pack(p[8 * t + 4], p[8 * t + 5]),
+                       T::pack(p[8 * t + 6], p[8 * t + 7])};
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          const char *x = lds + (from_now ^ 32 * i) + t * 32 * (2 * D);
+          const u32x2 v0 = read_transposed(x), v1 = read_transposed(x + 16 * (2 * D));  // r + 16: the same exchange
+          o[i] = T::mfma16(u32x4{v0.x, v0.y, v1.x, v1.y}, pw, o[i]);
+        }
       }
     }
     if (!one_token && __any(odd)) {
@@ -317,6 +336,7 @@ __global__ __launch_bounds__(64 * FW, at_once(D)) void few_kernel(AttendArgs a) 
             const f32x4 v = four_values<T, KV>(at, 16 * i + 4 * grp);
 #pragma unroll
             for (int k = 0; k < 4; ++k) o[i][k] = seen && !is_finite(v[k]) ? o[i][k] + v[k] : o[i][k];
+            __builtin_amdgcn_sched_barrier(0);  // (rare: in few registers)
           }
         }
       }
@@ -382,7 +402,7 @@ constexpr bool OTHER_SCORES = false;
 #endif
 template <typename T, Pages KV, int D>
 int launch_d(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
-  const dim3 grid(uint32_t(max_groups * a.n_kv)), block(64 * FW);
+  const dim3 grid(uint32_t(max_groups * a.n_kv)), block(64 * few_waves(KV, D));
   if (a.cache.ps.size % 16 == 0)
     few_kernel<T, KV, D, true, OTHER_SCORES><<<grid, block, 0, stream>>>(a);
   else

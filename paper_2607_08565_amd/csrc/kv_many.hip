@@ -95,12 +95,6 @@ __device__ __forceinline__ int value_swap(int row) {
 // cores take 32 cycles each for.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
-// x, computed again in every step: what follows from it is not kept in registers across them.
-__device__ __forceinline__ int again(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
 // What a wavefront keeps of its 32 rows; lane (half, col) holds row col's.
 template <int D>
 struct Rows {
@@ -474,8 +468,8 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
           vp = read_lane(at_l.v, from);
           if (KV4) {
             const uint32_t row = r % 16 + lrow, g = D == 64 ? lcol / 2 : lcol;
-            kx[i] = load_exp(read_lane(at_l.k_exp, from) + (row * uint32_t(a.cache.k_exp.token) + g));
-            vx[i] = load_exp(read_lane(at_l.v_exp, from) + (row * uint32_t(a.cache.v_exp.token) + g));
+            kx[i] = load_exp(read_lane(at_l.k_exp, from), (row * uint32_t(a.cache.k_exp.token) + g));
+            vx[i] = load_exp(read_lane(at_l.v_exp, from), (row * uint32_t(a.cache.v_exp.token) + g));
           }
           ko += k_lane + uint32_t(r % 16) * uint32_t(a.cache.k.token);
           vo += v_lane + uint32_t(r % 16) * uint32_t(a.cache.v.token);
@@ -493,8 +487,8 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
           }
         }
         if (KV != PAGES16) {
-          kr[i] = load_piece<PB>(kp + ko);
-          vr[i] = load_piece<PB>(vp + vo);
+          kr[i] = load_piece<PB>(kp, ko);
+          vr[i] = load_piece<PB>(vp, vo);
         } else if (WIDE) {
           to_lds(kp, ko, kl + r * ROWB, vp, vo, vl + r * ROWB);
         } else {
