@@ -170,11 +170,11 @@ __device__ __forceinline__ int again(int x) {
 // scale), the capped score, cap tanh(scale x / cap) = cap - 2 cap / (1 + exp(2 scale x / cap)): both ends
 // come out of the exponential's own overflow to infinity and underflow to zero.
 struct Capped {
-  float rate, cap;  // of the exponent, 2 sc / cap; cap log2(e)
-  __device__ __forceinline__ Capped(const AttendArgs &a, float sc)
-      : rate(a.cap_log2 > 0.0f ? 2.8853900817779268f * sc / a.cap_log2 : 0.0f), cap(a.cap_log2) {}
+  float rate, cap, top;  // of the exponent, 2 sc / cap; cap log2(e); that less m, which scores are taken from
+  __device__ __forceinline__ Capped(const AttendArgs &a, float sc, float m = 0.0f)
+      : rate(a.cap_log2 > 0.0f ? 2.8853900817779268f * sc / a.cap_log2 : 0.0f), cap(a.cap_log2), top(a.cap_log2 - m) {}
   __device__ __forceinline__ float operator()(float x) const {
-    return fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * rate)), cap);
+    return fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * rate)), top);
   }
 };
 constexpr float LOG2E = 1.4426950408889634f;

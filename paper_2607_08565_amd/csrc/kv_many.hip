@@ -127,13 +127,23 @@ struct Values {
   }
 };
 
+// What is done to a product before it is a score.  CAPPED: capped by so little that the weights need no
+// running maximum, with BF16, whose weights have float32's range: scores are then within cap of 0, and with
+// m = min(cap, 84 - cap) in powers of two, cap up to 73 (50.5 natural), weights are between 2^-84 and 2^62:
+// far from both ends also times values and summed over 2^24 keys.  That saves the maxima and a
+// subtraction, of eleven instructions a score two and a half (4,096 tokens over 16,384: CAPPED_US).
+enum Scores { PLAIN, CAPPED, OTHER };
+constexpr float CAPPED_MOST = 73.0f;
+__device__ __forceinline__ float capped_maximum(float cap) { return fminf(cap, 84.0f - cap); }
+
 // One step's 64 keys: the scores.  S^T: lane (half, col) gets row col's scores of keys kb +
 // 32 j + 8 (r / 4) + 4 half + r % 4, -inf for those that the row does not see (MASKED: there
-// may be some).  Returns the row's largest, and the first 16 keys' values on their way.  SCORES:
-// capped or with a bias by distance, in powers of two already.
-template <typename T, int D, bool MASKED, bool SCORES>
+// may be some).  Returns the row's largest, and the first 16 keys' values on their way.  Other
+// scores come out in powers of two already, but those with a bias alone: that is where the products'
+// sums begin, at no cost, unless dividing it by the factor to come would leave float32's range.
+template <typename T, int D, bool MASKED, Scores S>
 __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, const char *kl, const char *vl, int32_t kb,
-                                        float sc, int lane, f32x16 (&s)[2], Values<D> &first) {
+                                        float &sc, int lane, f32x16 (&s)[2], Values<D> &first) {
   constexpr int N = D / 8, AHEAD = 4, ROWB = 2 * D;
   const int l = again(lane), col = l & 31, swap = 16 * ((l >> 5) ^ key_swap<D>(col));
   const char *row = kl + col * ROWB;
@@ -143,10 +153,19 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, c
   u32x4 k[AHEAD];
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n) k[n] = piece(n);
+  const bool begin = S == OTHER && !(a.cap_log2 > 0.0f) && sc >= 0x1p-60f;
+  if (begin) {
+    const float slope = w.slope / sc, from = slope * float(kb + 4 * (lane >> 5) - (w.hi - 1));
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
+      for (int r = 0; r < 16; ++r) s[j][r] = fmaf(slope, float(32 * j + 8 * (r / 4) + r % 4), from);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
+  }
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     in_order();
@@ -157,7 +176,14 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, c
   in_order();
   __builtin_amdgcn_s_setprio(0);
   first.read(vl, Values<D>::offset(again(lane)), 0);
-  if (SCORES) {
+  if (S == CAPPED) {
+    const Capped capped(a, sc, capped_maximum(a.cap_log2));
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[j][r] = capped(s[j][r]);
+  }
+  if (S == OTHER && !begin) {
     if (a.cap_log2 > 0.0f) {
       const Capped capped(a, sc);
 #pragma unroll
@@ -190,6 +216,7 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, c
         if (key >= hi || key < lo) s[j][r] = -INFINITY;
       }
   }
+  if (S == CAPPED) return 0.0f;
   float mx = max3(s[0][0], s[0][1], s[1][0]);
 #pragma unroll
   for (int r = 2; r < 16; r += 2) mx = max3(mx, s[0][r], s[0][r + 1]);
@@ -205,7 +232,8 @@ __device__ __forceinline__ float exponent(const Rows<D> &w) {  // of weight 2^MA
 }
 
 // The products of 16 keys' weights with their values, among them the next 16's weights and reads.
-template <typename T, int D>
+// READY: the scores are the weights' exponents.
+template <typename T, bool READY, int D>
 __device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, int lane, const f32x16 (&s)[2],
                                          const Values<D> &first) {
   constexpr int DT = D / 32;
@@ -215,8 +243,9 @@ __device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, i
   u32x4 p[2];
   v[0] = first;
   const auto weights = [&](int t, int e) {
-    const float x = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e], sc, base));
-    const float y = __builtin_amdgcn_exp2f(fmaf(s[t / 2][8 * (t % 2) + 2 * e + 1], sc, base));
+    const float a = s[t / 2][8 * (t % 2) + 2 * e], b = s[t / 2][8 * (t % 2) + 2 * e + 1];
+    const float x = __builtin_amdgcn_exp2f(READY ? a : fmaf(a, sc, base));
+    const float y = __builtin_amdgcn_exp2f(READY ? b : fmaf(b, sc, base));
     w.l += x + y;
     p[t % 2][e] = T::pack(x, y);
   };
@@ -269,23 +298,25 @@ __device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown
 }
 
 // A step.  ENDS: not every row sees all of its keys.
-template <typename T, int D, bool ENDS, bool SCORES>
+template <typename T, int D, bool ENDS, Scores S>
 __device__ __forceinline__ void step(const AttendArgs &a, Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc,
                                      int lane) {
   f32x16 s[2];
   Values<D> first;
-  const float mx = scores<T, D, ENDS, SCORES>(a, w, kl, vl, kb, sc, lane, s, first);
-  const uint64_t grown = __ballot(mx > w.m + SLACK);  // also the first time: m is -inf
-  float down = 1.0f;
-  if (grown) {  // only the rows that have grown: another one's scores change nothing in a row
-    const bool mine = mx > w.m + SLACK;
-    down = mine ? __builtin_amdgcn_exp2f(w.m - mx) : 1.0f;
-    w.m = mine ? mx : w.m;
-    w.l *= down;
-  }
+  const float mx = scores<T, D, ENDS, S>(a, w, kl, vl, kb, sc, lane, s, first);
+  if (S != CAPPED) {
+    const uint64_t grown = __ballot(mx > w.m + SLACK);  // also the first time: m is -inf
+    float down = 1.0f;
+    if (grown) {  // only the rows that have grown: another one's scores change nothing in a row
+      const bool mine = mx > w.m + SLACK;
+      down = mine ? __builtin_amdgcn_exp2f(w.m - mx) : 1.0f;
+      w.m = mine ? mx : w.m;
+      w.l *= down;
+    }
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
-  products<T>(w, vl, SCORES ? 1.0f : sc, lane, s, first);
+    for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
+  }
+  products<T, S == CAPPED>(w, vl, sc, lane, s, first);
 }
 
 // A wavefront's rows: the output, or the sums for the joining.
@@ -354,7 +385,7 @@ __device__ __forceinline__ void add_not_finite(const AttendArgs &a, const PlanIt
 }
 
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
-template <typename T, Pages KV, int D, bool WIDE, bool SCORES>
+template <typename T, Pages KV, int D, bool WIDE, Scores S>
 __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
   constexpr bool KV8 = KV == PAGES8, KV4 = KV == PAGES4;
   constexpr int PB = KV4 ? piece4(D) : 16;  // bytes of a lane's load
@@ -395,7 +426,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     const int32_t first = it.kv_len - it.n_new;  // the first new token's place
     w.hi = has_row ? first + tok + 1 : 0;
     w.lo = a.window > 0 ? first + tok + 1 - a.window : 0;
-    w.slope = SCORES && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
+    w.slope = S == OTHER && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
     // the wavefront's first and last row, and the tile's
     const int32_t min_hi = first + row0 / a.group + 1;
     const int32_t max_hi = n_rows > 0 ? first + (row0 + n_rows - 1) / a.group + 1 : 0;
@@ -430,7 +461,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     for (int i = 0; i < DT; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) w.o[i][r] = 0.0f;
-    w.m = -INFINITY;
+    w.m = S == CAPPED ? capped_maximum(a.cap_log2) : -INFINITY;
     w.l = 0.0f;
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
 
@@ -567,7 +598,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
         load_next(kb);
         if (ENDS) look_over(kb, here() + SIDE);
         if (!ENDS || (n_rows > 0 && kb < max_hi && kb + KT > min_lo))
-          step<T, D, ENDS, SCORES>(a, w, here(), here() + SIDE, kb, sc, lane);
+          step<T, D, ENDS, S>(a, w, here(), here() + SIDE, kb, sc, lane);
         if (KV != PAGES16 && kb + KT < k1) to_16(there());
         arrived();
       }
@@ -607,19 +638,24 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
   }
 }
 
-#ifdef SCORED
-constexpr bool OTHER_SCORES = true;
-#else
-constexpr bool OTHER_SCORES = false;
-#endif
-template <typename T, Pages KV, int D>
-int launch_d(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
+template <typename T, Pages KV, int D, Scores S>
+int launch_s(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
   const dim3 grid(uint32_t(max_groups * a.n_kv)), block(MT);
   if (a.cache.ps.size % 16 == 0)
-    many_kernel<T, KV, D, true, OTHER_SCORES><<<grid, block, 0, stream>>>(a);
+    many_kernel<T, KV, D, true, S><<<grid, block, 0, stream>>>(a);
   else
-    many_kernel<T, KV, D, false, OTHER_SCORES><<<grid, block, 0, stream>>>(a);
+    many_kernel<T, KV, D, false, S><<<grid, block, 0, stream>>>(a);
   return hip_status(hipGetLastError());
+}
+template <typename T, Pages KV, int D>
+int launch_d(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
+#ifdef SCORED
+  if constexpr (std::is_same_v<T, Bf16>)
+    if (!a.slopes && a.cap_log2 <= CAPPED_MOST) return launch_s<T, KV, D, CAPPED>(a, max_groups, stream);
+  return launch_s<T, KV, D, OTHER>(a, max_groups, stream);
+#else
+  return launch_s<T, KV, D, PLAIN>(a, max_groups, stream);
+#endif
 }
 template <typename T, Pages KV>
 int launch_k(const AttendArgs &a, int32_t d, int64_t max_groups, hipStream_t stream) {
