@@ -102,7 +102,7 @@ struct Rows {
   f32x16 o[D / 32];  // O^T: components 32 i + 8 (r / 4) + 4 half + r % 4
   float m, l;        // of the half's keys (l), of all (m)
   int32_t hi, lo;    // the keys [lo, hi) that the row sees
-  float slope;       // other scores: the bias of a key's distance, in powers of two
+  float slope;       // other scores: a key's bias by distance, of the products' sums or in powers of two
 };
 
 // The values of 16 keys of a step, V^T as the matrix instruction takes it: read in the order in
@@ -127,83 +127,74 @@ struct Values {
   }
 };
 
-// What is done to a product before it is a score.  CAPPED: capped by so little that the weights need no
-// running maximum, with BF16, whose weights have float32's range: scores are then within cap of 0, and with
-// m = min(cap, 84 - cap) in powers of two, cap up to 73 (50.5 natural), weights are between 2^-84 and 2^62:
-// far from both ends also times values and summed over 2^24 keys.  That saves the maxima and a
-// subtraction, of eleven instructions a score two and a half (4,096 tokens over 16,384: CAPPED_US).
-enum Scores { PLAIN, CAPPED, OTHER };
+// What is done to a product before it is a score (smetric_attend_scores):
+//   BIASED  the bias, divided by the factor to come, is where the products' sums begin, instead of 0
+//   CAPPED  capped by so little that the weights need no running maximum, with BF16, whose weights have
+//           float32's range: scores are within cap of 0, and with m = min(cap, 84 - cap) in powers of
+//           two, cap up to 73 (50.5 natural), weights are between 2^-84 and 2^62: far from both ends
+//           also times values and summed over 2^24 keys.  That saves the maxima, a subtraction and the
+//           sums' scaling (2,048 tokens over 8,048: 195 us, without 175)
+//   OTHER   capped and, maybe, biased then
+// Capping takes five instructions a score, two of them at half rate, as long as the matrix cores take
+// for it at heads of 128: so the first 32 keys' scores are capped during the other 32's products, and
+// the others' (CAPPED) during those with the values (175 us, so 168).
+enum Scores { PLAIN, BIASED, CAPPED, OTHER };
 constexpr float CAPPED_MOST = 73.0f;
 __device__ __forceinline__ float capped_maximum(float cap) { return fminf(cap, 84.0f - cap); }
 
 // One step's 64 keys: the scores.  S^T: lane (half, col) gets row col's scores of keys kb +
 // 32 j + 8 (r / 4) + 4 half + r % 4, -inf for those that the row does not see (MASKED: there
-// may be some).  Returns the row's largest, and the first 16 keys' values on their way.  Other
-// scores come out in powers of two already, but those with a bias alone: that is where the products'
-// sums begin, at no cost, unless dividing it by the factor to come would leave float32's range.
+// may be some).  Returns the row's largest, and the first 16 keys' values on their way.
 template <typename T, int D, bool MASKED, Scores S>
 __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, const char *kl, const char *vl, int32_t kb,
-                                        float &sc, int lane, f32x16 (&s)[2], Values<D> &first) {
+                                        float sc, int lane, f32x16 (&s)[2], Values<D> &first) {
   constexpr int N = D / 8, AHEAD = 4, ROWB = 2 * D;
+  constexpr bool CAP = S == CAPPED || S == OTHER;
   const int l = again(lane), col = l & 31, swap = 16 * ((l >> 5) ^ key_swap<D>(col));
   const char *row = kl + col * ROWB;
   const auto piece = [&](int n) {  // (32 rows on: the same exchange)
-    return *reinterpret_cast<const u32x4 *>(row + ((n / 2 * 32) ^ swap) + n % 2 * (32 * ROWB));
+    const int j = CAP ? n / (N / 2) : n % 2, d = CAP ? n % (N / 2) : n / 2;
+    return *reinterpret_cast<const u32x4 *>(row + ((d * 32) ^ swap) + j * (32 * ROWB));
   };
   u32x4 k[AHEAD];
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n) k[n] = piece(n);
-  const bool begin = S == OTHER && !(a.cap_log2 > 0.0f) && sc >= 0x1p-60f;
-  if (begin) {
-    const float slope = w.slope / sc, from = slope * float(kb + 4 * (lane >> 5) - (w.hi - 1));
+  const float from = S == BIASED || S == OTHER ? w.slope * float(kb + 4 * (lane >> 5) - (w.hi - 1)) : 0.0f;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+  for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[j][r] = fmaf(slope, float(32 * j + 8 * (r / 4) + r % 4), from);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
-  }
+    for (int r = 0; r < 16; ++r) s[j][r] = S == BIASED ? fmaf(w.slope, float(32 * j + 8 * (r / 4) + r % 4), from) : 0.0f;
+  const Capped capped(a, sc, S == CAPPED ? capped_maximum(a.cap_log2) : 0.0f);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     in_order();
     if (n == 0) __builtin_amdgcn_s_setprio(1);
-    s[n % 2] = T::mfma32(k[n % AHEAD], w.q[n / 2], s[n % 2]);
+    if (CAP)
+      s[n / (N / 2)] = T::mfma32(k[n % AHEAD], w.q[n % (N / 2)], s[n / (N / 2)]);
+    else
+      s[n % 2] = T::mfma32(k[n % AHEAD], w.q[n / 2], s[n % 2]);
     if (n + AHEAD < N) k[n % AHEAD] = piece(n + AHEAD);
+    // the first 32 keys' scores during the others' products
+    constexpr int PER = 32 / N;
+    if (CAP && n > N / 2)
+#pragma unroll
+      for (int r = PER * (n - N / 2 - 1); r < PER * (n - N / 2); ++r) s[0][r] = capped(s[0][r]);
   }
   in_order();
   __builtin_amdgcn_s_setprio(0);
   first.read(vl, Values<D>::offset(again(lane)), 0);
-  if (S == CAPPED) {
-    const Capped capped(a, sc, capped_maximum(a.cap_log2));
+  if (CAP) {
+#pragma unroll
+    for (int r = 16 - 32 / N; r < 16; ++r) s[0][r] = capped(s[0][r]);
+    if (S == OTHER || MASKED)  // (the others' among the products with the values: products)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[1][r] = capped(s[1][r]);
+  }
+  if (S == OTHER && a.slopes) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[j][r] = capped(s[j][r]);
-  }
-  if (S == OTHER && !begin) {
-    if (a.cap_log2 > 0.0f) {
-      const Capped capped(a, sc);
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[j][r] = capped(s[j][r]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[j][r] *= sc;
-    }
-    if (a.slopes) {
-      const float from = w.slope * float(kb + 4 * (lane >> 5) - (w.hi - 1));
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[j][r] += fmaf(w.slope, float(32 * j + 8 * (r / 4) + r % 4), from);
-    }
-    sc = 1.0f;
+      for (int r = 0; r < 16; ++r) s[j][r] += fmaf(w.slope, float(32 * j + 8 * (r / 4) + r % 4), from);
   }
   if (MASKED) {
     const int half = lane >> 5;
@@ -224,7 +215,7 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, c
   for (int r = 1; r < 15; r += 2) mx = max3(mx, s[1][r], s[1][r + 1]);
   mx = __builtin_elementwise_maximum(mx, s[1][15]);
   const u32x2 both = swap32(__float_as_uint(mx), __float_as_uint(mx));
-  return __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * sc;
+  return __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * (S == OTHER ? 1.0f : sc);
 }
 template <typename T, int D>
 __device__ __forceinline__ float exponent(const Rows<D> &w) {  // of weight 2^MANY_SHIFT
@@ -232,20 +223,22 @@ __device__ __forceinline__ float exponent(const Rows<D> &w) {  // of weight 2^MA
 }
 
 // The products of 16 keys' weights with their values, among them the next 16's weights and reads.
-// READY: the scores are the weights' exponents.
-template <typename T, bool READY, int D>
-__device__ __forceinline__ void products(Rows<D> &w, const char *vl, float sc, int lane, const f32x16 (&s)[2],
-                                         const Values<D> &first) {
+// Capped scores are the weights' exponents, the last 32 keys' (LATER) after capping, which is done here.
+template <typename T, bool CAP, bool LATER, int D>
+__device__ __forceinline__ void products(const AttendArgs &a, Rows<D> &w, const char *vl, float sc, int lane,
+                                         const f32x16 (&s)[2], const Values<D> &first) {
   constexpr int DT = D / 32;
   const float base = exponent<T>(w);
+  const Capped capped(a, sc, CAP ? capped_maximum(a.cap_log2) : 0.0f);
   const int off = Values<D>::offset(again(lane));
   Values<D> v[2];
   u32x4 p[2];
   v[0] = first;
   const auto weights = [&](int t, int e) {
-    const float a = s[t / 2][8 * (t % 2) + 2 * e], b = s[t / 2][8 * (t % 2) + 2 * e + 1];
-    const float x = __builtin_amdgcn_exp2f(READY ? a : fmaf(a, sc, base));
-    const float y = __builtin_amdgcn_exp2f(READY ? b : fmaf(b, sc, base));
+    const auto weight = [&](float z) {
+      return __builtin_amdgcn_exp2f(!CAP ? fmaf(z, sc, base) : LATER && t >= 2 ? capped(z) : z);
+    };
+    const float x = weight(s[t / 2][8 * (t % 2) + 2 * e]), y = weight(s[t / 2][8 * (t % 2) + 2 * e + 1]);
     w.l += x + y;
     p[t % 2][e] = T::pack(x, y);
   };
@@ -316,7 +309,7 @@ __device__ __forceinline__ void step(const AttendArgs &a, Rows<D> &w, const char
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
   }
-  products<T, S == CAPPED>(w, vl, sc, lane, s, first);
+  products<T, S == CAPPED, !ENDS>(a, w, vl, S == OTHER ? 1.0f : sc, lane, s, first);
 }
 
 // A wavefront's rows: the output, or the sums for the joining.
@@ -426,7 +419,6 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     const int32_t first = it.kv_len - it.n_new;  // the first new token's place
     w.hi = has_row ? first + tok + 1 : 0;
     w.lo = a.window > 0 ? first + tok + 1 - a.window : 0;
-    w.slope = S == OTHER && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
     // the wavefront's first and last row, and the tile's
     const int32_t min_hi = first + row0 / a.group + 1;
     const int32_t max_hi = n_rows > 0 ? first + (row0 + n_rows - 1) / a.group + 1 : 0;
@@ -449,6 +441,12 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
         sc = sc < 0.0f ? -sc : sc == 0.0f ? 0x1p-126f : 1.0f;
       }
     }
+    // A bias divided by the factor stays in float32's range: where that is next to nothing, it takes
+    // 2^66 of the queries (F16's become zeros: their scores are below 2^-20).
+    const float smaller = S == BIASED && sc < 0x1p-60f ? 0x1p-66f : 1.0f;
+    sc /= smaller;
+    w.slope = (S == BIASED || S == OTHER) && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
+    if (S == BIASED) w.slope /= sc;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       w.q[s] = u32x4{0, 0, 0, 0};
@@ -456,6 +454,9 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
         w.q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + s * 16 +
                                                   half * 8);
       if (KV8) w.q[s] = (w.q[s] ^ flip) | nan;
+      if (S == BIASED && smaller != 1.0f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w.q[s][e] = T::pack(T::lo(w.q[s][e]) * smaller, T::hi(w.q[s][e]) * smaller);
     }
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -652,6 +653,7 @@ int launch_d(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
 #ifdef SCORED
   if constexpr (std::is_same_v<T, Bf16>)
     if (!a.slopes && a.cap_log2 <= CAPPED_MOST) return launch_s<T, KV, D, CAPPED>(a, max_groups, stream);
+  if (!(a.cap_log2 > 0.0f)) return launch_s<T, KV, D, BIASED>(a, max_groups, stream);
   return launch_s<T, KV, D, OTHER>(a, max_groups, stream);
 #else
   return launch_s<T, KV, D, PLAIN>(a, max_groups, stream);
