@@ -73,6 +73,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
   // asked for together: a workgroup's start is a chain of round trips
   const PlanHdr hdr = *a.hdr;
   const int32_t first_piece = uniform(a.first[share]), last_piece = uniform(a.first[share + 1]);
+  const PlanItem guess = uniform(a.items[share]);  // the first piece of a share, where tiles do not end inside one before
   if (!plan_fits(a, hdr)) {
     write_nothing<D>(a);
     return;
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
   for (int32_t piece = first_piece; piece < last_piece; ++piece) {
-    const PlanItem it = uniform(a.items[piece]);
+    const PlanItem it = piece == share ? guess : uniform(a.items[piece]);
     const int32_t row0 = it.tile * FEW_ROWS;
     int32_t n_rows = it.n_new * a.group - row0;
     if (n_rows > FEW_ROWS) n_rows = FEW_ROWS;

@@ -246,13 +246,15 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   constexpr int TPP = D / 4, SIDE = 256 / TPP, BLOCKS = FEW ? FEW_ROWS : MANY_ROWS / SIDE;
   __shared__ f32x4 sh[256];
   __shared__ float shl[SIDE];
+  // a short request's joining is a chain of round trips: the first unit's split is asked for with the header
+  PlanSplit s = a.splits[blockIdx.x / a.n_kv / BLOCKS];
   const PlanHdr h = *a.hdr;
   if (!plan_fits(a, h)) return;
   const int64_t units = int64_t(h.n_splits) * a.n_kv * BLOCKS;
   const int32_t sub = threadIdx.x % TPP, side = threadIdx.x / TPP;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int32_t kvh = int32_t(u % a.n_kv), block = int32_t(u / a.n_kv % BLOCKS);
-    const PlanSplit s = a.splits[u / a.n_kv / BLOCKS];
+    if (u != blockIdx.x) s = a.splits[u / a.n_kv / BLOCKS];
     const int32_t row = FEW ? block : block * SIDE + side;
     const int32_t in_req = s.tile * a.rows + row;
     const int64_t step = int64_t(a.n_kv) * a.rows, at = (int64_t(s.part0) * a.n_kv + kvh) * a.rows + row;
@@ -260,6 +262,10 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     const f32x2 *ml = a.parts.ml + at;
     const float *parts = a.parts.acc + at * D + sub * 4;
     float m = -INFINITY;
+    // (few rows: a side's first part is asked for with the maxima)
+    const bool has = FEW && side < s.n_parts;
+    const f32x2 ml0 = has ? ml[side * step] : f32x2{-INFINITY, 0.0f};
+    const f32x4 v0 = has ? *reinterpret_cast<const f32x4 *>(parts + side * step * D) : f32x4{0, 0, 0, 0};
     if (FEW) {
       for (int32_t p = threadIdx.x & 63; p < s.n_parts; p += 64) m = fmaxf(m, ml[p * step].x);
 #pragma unroll
@@ -270,8 +276,13 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     const float ms = m == -INFINITY ? 0.0f : m;
     f32x4 acc{0, 0, 0, 0};
     float l = 0.0f;
+    if (has) {
+      const float w = exp2f(ml0.x - ms);
+      l = w * ml0.y;
+      acc = f32x4{w * v0[0], w * v0[1], w * v0[2], w * v0[3]};
+    }
 #pragma unroll 4
-    for (int32_t p = FEW ? side : 0; p < s.n_parts; p += FEW ? SIDE : 1) {
+    for (int32_t p = FEW ? side + SIDE : 0; p < s.n_parts; p += FEW ? SIDE : 1) {
       const f32x2 x = ml[p * step];
       const f32x4 v = *reinterpret_cast<const f32x4 *>(parts + p * step * D);
       const float w = exp2f(x.x - ms);
