@@ -146,12 +146,6 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, const int32_t *t
 // What a lane takes of a row of E2M1 at once: 16 bytes, a group with one exponent; of the 32 bytes of
 // a head of 64 half a group, so that 16 rows are a wavefront's load as with the others.
 constexpr int piece4(int head_dim) { return head_dim == 64 ? 8 : 16; }
-// From an address that is known to be memory's: a load that might be LDS's counts as one of both, and
-// then every read of LDS waits for the keys and values on their way.
-template <typename V>
-__device__ __forceinline__ V from_memory(uint64_t p, uint32_t offset = 0) {
-  return *(const __attribute__((address_space(1))) V *)((const __attribute__((address_space(1))) char *)p + offset);
-}
 template <int BYTES>
 __device__ __forceinline__ u32x4 load_piece(uint64_t p, uint32_t offset = 0) {
   if (BYTES == 16) return from_memory<u32x4>(p, offset);

@@ -138,6 +138,13 @@ struct HeadsView {  // strides in elements of 16 bits
   int64_t token, head;
 };
 
+// From an address that is known to be memory's: a load that might be LDS's counts as one of both, and
+// then every read of LDS waits for the keys and values on their way.
+template <typename V>
+__device__ __forceinline__ V from_memory(uint64_t p, uint32_t offset = 0) {
+  return *(const __attribute__((address_space(1))) V *)((const __attribute__((address_space(1))) char *)p + offset);
+}
+
 // The request of a token t, the last r with q_off[r] <= t, and its numbers.
 struct Request {
   int32_t r, len;    // kv_len
