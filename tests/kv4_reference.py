@@ -81,7 +81,8 @@ def attend(q, keys, values_, n_kv, scale, window, kv_len, n_new, cap=0.0, slopes
             p = torch.exp(s - lse[i, h])
             out[i, h], mag[i, h] = p @ vv, p @ vv.abs()
             big[i, h] = scale * (kk.abs() @ q[i, h].abs()).max()
-            more[i, h] = cap * 2.0 ** -20 + (0 if slopes is None else slopes[h].double().abs() * (place - lo) * 2.0 ** -22)
+            bias = 0 if slopes is None else slopes[h].double().abs() * (place - lo)
+            more[i, h] = cap * 2.0 ** -20 + bias * (D / 16 + 8) * ref.F32
     return out, lse, mag, big, more
 
 
@@ -91,9 +92,10 @@ def close_scores(out, lse, want, dim, dtype):
     A cap: t = 1 - 2 / (1 + e), e = 2^y.  y has five roundings, y 2^-24 each, which reach t through
     2 e / (1 + e)^2 y ln 2 <= 0.45: 2.3 units of 2^-24; e's own last place 1, the sum 1, the reciprocal's
     last place 4, the last product and sum 2, the factors log2(e) 1: below 12, 2^-20 has 16.
-    A bias: slope log2(e), its product with the distance, the products' sum and its sum with the
-    score, each a rounding of at most twice the bias: 8 units of 2^-24, 2^-22 has 4 -- of a base
-    and a step whose sum is the bias itself, so two of them count once."""
+    A bias: slope log2(e), that divided by the score's factor, the product with the first key's distance,
+    the sum with the key's own, the factor's and the last product's and sum's roundings: 8 of at most the
+    bias, 2^-24 each.  In chunks it is where the sum of the products begins, dim / 16 matrix
+    products, each of which rounds the sum so far: as many more."""
     o, l, mag, big, more = want
     # products of dim terms and, beside them, what the running maximum's subtraction rounds
     score = big * dim * ref.F32 + more
