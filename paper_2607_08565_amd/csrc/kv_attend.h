@@ -154,6 +154,15 @@ __device__ __forceinline__ u32x4 load_piece(uint64_t p, uint32_t offset = 0) {
 }
 __device__ __forceinline__ uint32_t load_exp(uint64_t p, uint32_t offset = 0) { return from_memory<uint8_t>(p, offset); }
 
+// The four words of a lane's load of 4-bit components in the order in which they, widened, go to LDS as its
+// 16-byte pieces: word n ^ flip as the n-th.  A write of 16 bytes a lane takes 8 lanes at a time (as the
+// counters of conflicts say), which meet no bank twice if their pieces differ modulo 128 bytes:
+// neighbouring lanes' pieces are 4 apart, and rows' exchanges alone leave some of them on one another.
+__device__ __forceinline__ u32x4 flipped(u32x4 x, int flip) {
+  x = flip & 2 ? u32x4{x.z, x.w, x.x, x.y} : x;
+  return flip & 1 ? u32x4{x.y, x.x, x.w, x.z} : x;
+}
+
 // x, computed again in every step: what follows from it is not kept in registers across them.
 __device__ __forceinline__ int again(int x) {
   asm volatile("" : "+v"(x));

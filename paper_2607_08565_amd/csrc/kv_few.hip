@@ -17,7 +17,12 @@
 //
 // Measured: 32 requests decoding over 1.73 GB of cache 305 us, 5.7 TB/s (a copy of 4 GiB moves
 // 4.8); 64 drafted tokens over 0.58 GB 117 us; 131,072 keys of 8 bits (134 MB) 31 to 35 us, 24
-// of them here and the rest the joining; a lone token over 1,025 keys 9.5 us, two launches.
+// of them here and the rest the joining; a lone token over 1,025 keys 9.4 us, two launches.
+// 4 bits, where a lane's 16 bytes are a group of 32 components, widened two at an instruction with its
+// exponent: the 32 requests (0.41 GB) 85 us, 4.8 TB/s, of which the kernel has 79, 5.2 TB/s; a lone
+// token 8.8; 131,072 keys 24; 32 requests over 16,384 at heads of 64 70, over 8,192 at heads of 256, one
+// wavefront a SIMD, 80.  Scores that are capped take 4 instructions more, two of them at half
+// rate: at heads of 256 16 requests decoding over 1.33 GB 233 us, 5.7 TB/s; over the 4-bit pages of 32 99.
 #include <math.h>
 
 #include "kv_attend.h"
@@ -122,7 +127,8 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
     // computed here; a load's and a piece's share is exchanged in (its bits lie within a row).
     constexpr int PIECES = 2 * D / 16 / VROW;  // 16-byte pieces in LDS of a lane's load
     const int r0 = lane / VROW, tr = 4 * grp + col / 4;
-    const int to = wave * REGION + r0 * (2 * D) + ((PIECES * (lane % VROW)) ^ (2 * (r0 & SWZ))) * 16;
+    const int flip = !KV4 ? 0 : D == 64 ? r0 & 1 : lane % VROW >> 1;  // (flipped)
+    const int to = wave * REGION + r0 * (2 * D) + ((PIECES * (lane % VROW) + flip) ^ (2 * (r0 & SWZ))) * 16;
     const int from_t = wave * REGION + tr * (2 * D) + (((col % 4) / 2) ^ (2 * (tr & SWZ))) * 16 + (col & 1) * 8;
 
     const int32_t kb0 = k0 / KEY_STEP * KEY_STEP + FK * wave;
@@ -235,7 +241,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
       const int to_now = KV4 ? again(to) : to, from_now = KV4 ? again(from_t) : from_t;
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
-        u32x4 v = vr[i], w[PIECES];
+        u32x4 v = KV4 ? flipped(vr[i], flip) : vr[i], w[PIECES];
         uint32_t e = KV4 ? vx[i] : 0;
         if (partial && (kb + i * VRPI + r0 < k0 || kb + i * VRPI + r0 >= k1)) {
           v = u32x4{0, 0, 0, 0};

@@ -22,6 +22,12 @@
 // clock that falls under the load (1.9 GHz).  With the keys always in the nearest cache it takes
 // 5 % less, without the exponentials 8 %, without the maximum 5 %.  Heads of 64 do half the
 // products for the same weights: 24 requests with up to 1,000 new tokens 108 to 112 us, 370 to 383 TFLOP/s.
+//
+// 8- and 4-bit keys and values are widened on the way to LDS, 4-bit ones two at an instruction with their
+// group's exponent, once for the 128 rows: over 4-bit pages the same 4,096 tokens take 916 to 954 us, and 2
+// chunks of 2,048 at heads of 256 309.  Scores that are capped or biased: enum Scores.  Capped, BF16,
+// 4,096 over 16,384: 1,061 to 1,110 us, F16 1,180 to 1,224; biased 989 to 1,035; 2,048 over 8,048 with a
+// window of 4,096 capped 167 to 175.
 #include <math.h>
 
 #include <type_traits>
@@ -88,6 +94,17 @@ __device__ __forceinline__ int key_swap(int row) {
 template <int D>
 __device__ __forceinline__ int value_swap(int row) {
   return D == 64 ? 4 * (row >> 1 & 1) : 4 * (row & 3);
+}
+
+// Which of a lane's pieces of 4 bits goes there first (flipped): so that 8 lanes' pieces, of one or two rows, lie
+// in 8 places of 128 bytes.  Without, 118 of 295 M cycles of LDS are conflicts (4,096 tokens over 16,384: 938 us, so
+// 919; 2 chunks of 2,048 at heads of 256 348 us, so 309; at heads of 64, 2 to a place at most, 264 and 266).
+// 8-bit pieces, where it takes away conflicts as well, it makes slower (2 chunks of 2,048: 221 us, so 230).
+template <int D, bool VALUES>
+__device__ __forceinline__ int flip_of(int row, int lane_col) {
+  if (D == 64) return row & 1;
+  if (D == 256) return lane_col >> 1;
+  return (VALUES ? row & 1 : 0) ^ 2 * (lane_col >> 1);  // (keys: their rows' exchange is by one already)
 }
 
 // The order in which a wavefront's instructions are issued is the order of the source between
@@ -533,19 +550,20 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int r = i * RPL + wave * RPW + lrow;
+        const int fk = flip_of<D, false>(r, lcol), fv = flip_of<D, true>(r, lcol);
+        const u32x4 k = KV4 ? flipped(kr[i], fk) : kr[i], v = KV4 ? flipped(vr[i], fv) : vr[i];
         if (KV4) {
           constexpr int N = PB / 4;
           const float ke = power_of(kx[i]), ve = power_of(vx[i]);
 #pragma unroll
           for (int n = 0; n < N; ++n) {
-            *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((N * lcol + n) ^ key_swap<D>(r)) * 16) = T::eight_e2m1(kr[i][n], ke);
-            *reinterpret_cast<u32x4 *>(vl + r * ROWB + ((N * lcol + n) ^ value_swap<D>(r)) * 16) = T::eight_e2m1(vr[i][n], ve);
+            *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((N * lcol + (n ^ fk)) ^ key_swap<D>(r)) * 16) = T::eight_e2m1(k[n], ke);
+            *reinterpret_cast<u32x4 *>(vl + r * ROWB + ((N * lcol + (n ^ fv)) ^ value_swap<D>(r)) * 16) = T::eight_e2m1(v[n], ve);
           }
           continue;
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const u32x4 k = kr[i], v = vr[i];
           const uint32_t x = h ? k.z : k.x, y = h ? k.w : k.y, z = h ? v.z : v.x, u = h ? v.w : v.y;
           *reinterpret_cast<u32x4 *>(kl + r * ROWB + ((2 * lcol + h) ^ key_swap<D>(r)) * 16) =
               u32x4{T::template from_e4m3<false>(x), T::template from_e4m3<true>(x), T::template from_e4m3<false>(y),
