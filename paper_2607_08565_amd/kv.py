@@ -152,8 +152,8 @@ def qk_rotate(q: torch.Tensor, k: torch.Tensor, rotary: Rotary, positions: torch
 def append(cache: PagedCache, page_table: torch.Tensor, q_off: torch.Tensor, kv_len: torch.Tensor, k: torch.Tensor,
            v: torch.Tensor, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
            rotary: Rotary | None = None, positions: torch.Tensor | None = None, status: torch.Tensor | None = None):
-    """smetric_kv_append: the new tokens' keys (normed and rotated) and values into the pages;
-    kv_len counts the new tokens already.  With q its queries normed and rotated are
+    """smetric_kv_append: the new tokens' keys (normed and rotated) and values into the pages, quantised
+    where these hold 8 or 4 bits; kv_len counts the new tokens already.  With q its queries normed and rotated are
     returned (q_out, may be q)."""
     if q is not None and q_out is None:
         q_out = _new(q, "q")

@@ -92,6 +92,51 @@ def test_queries_that_are_not_finite(how, lens):
     assert torch.equal(got, out) and torch.equal(lse2, lse)
 
 
+@pytest.mark.parametrize("side", [0, 1])
+def test_read_one_side(side):
+    """Through the C entry point one side may be left out: it is not written, the other is what both give."""
+    import ctypes as C
+    import struct
+    from paper_2607_08565_amd import smetric as S
+    b = batch([(40, 40), (7, 9)], 2, 2, 64, BF, "fp4", seed=36)
+    both = _kv().read(b.cache, b.table, b.q_off, b.kv_len, b.T, BF)
+    out = torch.full((b.T, 2, 64), 5.0, dtype=BF, device="cuda")
+    heads = struct.pack("Pqq", out.data_ptr(), 128, 64)
+    where = struct.pack("PqiiPPq", b.table.data_ptr(), b.table.stride(0), b.table.shape[1], 2, b.q_off.data_ptr(),
+                        b.kv_len.data_ptr(), b.T)
+    stream = C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert S._lib.smetric_kv_read(0, b.cache.ref, where, *((heads, None) if side == 0 else (None, heads)), None, stream) == S.OK
+    assert torch.equal(out, both[side])
+
+
+@pytest.mark.parametrize("pages", ["same", "fp8", "fp4"])
+@pytest.mark.parametrize("how", [{}, dict(cap=20.0), dict(slopes=True)])
+@pytest.mark.parametrize("lens", [[(40, 2), (50, 1)], [(40, 40), (50, 33)]])
+def test_bad_batches(pages, how, lens):
+    """A page outside the cache, a request longer than its row, a plan of other lengths: status, no access
+    out of bounds, and the other request's rows as they were."""
+    kv, c = _kv(), batch(lens, 4, 2, 64, BF, pages, seed=37, **how)
+    slopes = None if c.slopes is None else c.slopes.cuda()
+    n, q, (good, good_lse) = lens[0][1], c.q.cuda(), c.run()
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def run(table, kv_len, q_off=c.q_off):
+        st.zero_()
+        lse = torch.zeros(c.T, 4, device="cuda")
+        plan = c.plan().make(q_off, kv_len)
+        out = kv.attend(q, c.cache, table, plan, lse=lse, status=st, cap=c.cap, slopes=slopes)
+        assert st.item() == -1
+        return out, lse
+    bad = c.table.clone()
+    bad[0, 1] = -1
+    out, lse = run(bad, c.kv_len)
+    assert torch.equal(out[n:], good[n:]) and torch.equal(lse[n:], good_lse[n:])
+    out, lse = run(c.table, torch.tensor([65, 50], dtype=torch.int32, device="cuda"))
+    assert bool((out[:n] == 0).all()) and bool((lse[:n] == -math.inf).all()) and torch.equal(out[n:], good[n:])
+    out, lse = run(c.table, torch.tensor([-1, 50], dtype=torch.int32, device="cuda"))
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
 def test_streams_at_once():
     """Steps with caches, plans and streams of their own, enqueued together, give what they give alone."""
     kv, many = _kv(), []
