@@ -99,7 +99,7 @@ __device__ __forceinline__ int value_swap(int row) {
 // Which of a lane's pieces of 4 bits goes there first (flipped): so that 8 lanes' pieces, of one or two rows, lie
 // in 8 places of 128 bytes.  Without, 118 of 295 M cycles of LDS are conflicts (4,096 tokens over 16,384: 938 us, so
 // 919; 2 chunks of 2,048 at heads of 256 348 us, so 309; at heads of 64, 2 to a place at most, 264 and 266).
-// 8-bit pieces, where it takes away conflicts as well, it makes slower (2 chunks of 2,048: 221 us, so 230).
+// 8-bit pieces, where it takes away conflicts as well, it makes slower (2 chunks of 2,048: 221 us, so 230; at heads of 256 317 both).
 template <int D, bool VALUES>
 __device__ __forceinline__ int flip_of(int row, int lane_col) {
   if (D == 64) return row & 1;

@@ -3,7 +3,9 @@
 //
 // The plan depends on the lengths alone, so one serves all layers of a step.  One workgroup
 // makes it: it totals the tiles' costs (key steps, and what a tile costs besides), decides on
-// shares or whole tiles, and every tile writes its pieces at places from scans over the tiles.
+// shares or whole tiles, and every tile's thread writes its pieces at places from scans over the tiles,
+// all threads together those of tiles that are cut often: 8 to 11 us also where one request of
+// 131,072 tokens is all that is cut (34 us by the tile's thread alone).
 #include <math.h>
 
 #include "kv_attend.h"
@@ -13,6 +15,8 @@ namespace {
 
 constexpr int PT = 512;
 constexpr int32_t STAGED = 2048;   // requests whose offsets and lengths are kept in LDS
+constexpr int32_t LONG_CUTS = 8;   // cuts of a tile, of which there are fewer than `target` in all, at most 512
+constexpr int32_t MAX_LONG = 512 / LONG_CUTS;
 constexpr int32_t CUT_COST = 8;    // steps: what a share's partial results cost, see whole_tiles (12: up to 7 % slower)
 
 struct PlanArgs {
@@ -107,13 +111,35 @@ __device__ bool whole_tiles(int64_t cost, int64_t tiles, int32_t longest, int32_
   return whole <= share + CUT_COST;
 }
 
+// A tile's pieces and the workgroups whose shares begin in it, written by threads i, i + step, ...:
+// shares' ends at multiples of `share`, of which w_lo .. w_hi cut the tile, whose costs begin at `at`.
+struct Cut {
+  Tile t;
+  int32_t cuts, cost;
+  int64_t at, w_lo, base, part0;
+};
+__device__ void write_pieces(const PlanArgs &a, const Cut &c, int64_t share, int64_t n_groups, int32_t i0, int32_t step) {
+  const Tile &t = c.t;
+  const int32_t k = t.k0 / KEY_STEP;
+  for (int32_t i = i0; i <= c.cuts && c.base + i < a.max_items; i += step) {
+    const int32_t c0 = i ? int32_t((c.w_lo + i - 1) * share - c.at) - a.tile_cost : 0;
+    const int32_t c1 = i < c.cuts ? int32_t((c.w_lo + i) * share - c.at) - a.tile_cost : 0;
+    a.items[c.base + i] = PlanItem{t.req, t.tok0, t.n_new, t.kv_len, t.tile, i == 0 ? t.k0 : (k + c0) * KEY_STEP,
+                                   i == c.cuts ? t.k1 : (k + c1) * KEY_STEP, c.cuts ? int32_t(c.part0 + i) : -1};
+  }
+  for (int64_t w = quotient(c.at + share - 1, share) + i0; w * share < c.at + c.cost && w < n_groups && w < a.max_groups; w += step)
+    a.first[w] = int32_t(c.base + (w < c.w_lo ? 0 : w > c.w_lo + c.cuts - 1 ? c.cuts + 1 : w - c.w_lo + 1));
+}
+
 __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
   static_assert(FEW_ROWS == 1 << 4 && MANY_ROWS == 1 << 7, "rows_log2");
   __shared__ int64_t sh64[PT / 64];
   __shared__ int64_t off_l[STAGED + 1];
   __shared__ int32_t len_l[STAGED];
-  __shared__ int bad, longest;
-  if (threadIdx.x == 0) bad = longest = 0;
+  // tiles of many pieces, which all threads write together (one thread's 130 of a long request take it 25 us)
+  __shared__ Cut cuts_l[MAX_LONG];
+  __shared__ int bad, longest, n_long;
+  if (threadIdx.x == 0) bad = longest = n_long = 0;
   __syncthreads();
   bool wrong = false;
   const bool staged = a.n_req <= STAGED;
@@ -184,21 +210,24 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
       int64_t all_n;
       const int64_t n = scan(int64_t(pieces) << 32 | int64_t(cuts ? pieces : 0) << 16 | (cuts > 0), all_n, sh64);
       const int64_t base = n_items + (n >> 32), part0 = n_parts + (n >> 16 & 0xFFFF), split_at = n_splits + (n & 0xFFFF);
-      const int32_t k = t.k0 / KEY_STEP;
-      for (int32_t i = 0; i < pieces && base + i < a.max_items; ++i) {
-        const int32_t c0 = i ? int32_t((w_lo + i - 1) * share - at) - a.tile_cost : 0;
-        const int32_t c1 = i < cuts ? int32_t((w_lo + i) * share - at) - a.tile_cost : 0;
-        a.items[base + i] = PlanItem{t.req, t.tok0, t.n_new, t.kv_len, t.tile, i == 0 ? t.k0 : (k + c0) * KEY_STEP,
-                                     i == cuts ? t.k1 : (k + c1) * KEY_STEP, cuts ? int32_t(part0 + i) : -1};
-      }
       if (cuts && split_at < a.max_splits)
         a.splits[split_at] = PlanSplit{t.tok0, t.n_new, t.tile, int32_t(part0), pieces, {0, 0, 0}};
       if (t.req >= 0 && whole) {
+        if (base < a.max_items) a.items[base] = PlanItem{t.req, t.tok0, t.n_new, t.kv_len, t.tile, t.k0, t.k1, -1};
         if (base < a.max_groups) a.first[base] = int32_t(base);
-      } else if (t.req >= 0) {  // the workgroups whose shares begin in this tile
-        for (int64_t w = quotient(at + share - 1, share); w * share < at + c && w < n_groups && w < a.max_groups; ++w)
-          a.first[w] = int32_t(base + (w < w_lo ? 0 : w > w_hi ? pieces : w - w_lo + 1));
+      } else if (t.req >= 0) {
+        // (w_lo as the divisions above give it also where nothing is cut: `first` goes by it)
+        const Cut cut{t, cuts, int32_t(c), at, w_lo, base, part0};
+        if (cuts < LONG_CUTS)
+          write_pieces(a, cut, share, n_groups, 0, 1);
+        else
+          cuts_l[atomicAdd(&n_long, 1)] = cut;
       }
+      __syncthreads();
+      const int32_t longs = n_long;
+      for (int32_t i = 0; i < longs; ++i) write_pieces(a, cuts_l[i], share, n_groups, threadIdx.x, PT);
+      __syncthreads();
+      if (threadIdx.x == 0) n_long = 0;  // (the next scan's barriers come before it is counted on)
       n_items += all_n >> 32;
       n_parts += all_n >> 16 & 0xFFFF;
       n_splits += all_n & 0xFFFF;
@@ -229,7 +258,8 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
 // Joins the parts of a cut tile: out = sum_p 2^(m_p - m) acc_p / sum_p 2^(m_p - m) l_p, in the
 // order of the parts.  D / 4 threads hold a row.  Tiles of many rows: the workgroup takes as
 // many rows at once (each of a few parts).  Tiles of few rows, which may have hundreds of
-// parts: it takes one row's parts side by side.
+// parts, and of many where a few long requests share all of the parts: it takes one row's parts
+// side by side (2 requests of 7 new tokens over 47,760, 14 heads on 2: 44 us, so 7).
 constexpr int32_t JOIN_GRID = 2048;
 template <typename T, int D, bool FEW>
 __device__ __forceinline__ void write_row(const AttendArgs &a, const PlanSplit &s, int32_t in_req, int32_t kvh, int sub,
@@ -250,23 +280,27 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   PlanSplit s = a.splits[blockIdx.x / a.n_kv / BLOCKS];
   const PlanHdr h = *a.hdr;
   if (!plan_fits(a, h)) return;
-  const int64_t units = int64_t(h.n_splits) * a.n_kv * BLOCKS;
+  const int64_t tiles = int64_t(h.n_splits) * a.n_kv;
+  const bool alone = FEW || tiles * MANY_ROWS <= gridDim.x;  // a row a workgroup, all at once
+  const int32_t blocks_log2 = __builtin_ctz(!FEW && alone ? MANY_ROWS : BLOCKS);
+  const int64_t units = tiles << blocks_log2;
   const int32_t sub = threadIdx.x % TPP, side = threadIdx.x / TPP;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int32_t kvh = int32_t(u % a.n_kv), block = int32_t(u / a.n_kv % BLOCKS);
-    if (u != blockIdx.x) s = a.splits[u / a.n_kv / BLOCKS];
-    const int32_t row = FEW ? block : block * SIDE + side;
+    const int64_t in_tile = u / a.n_kv;
+    const int32_t kvh = int32_t(u - in_tile * a.n_kv), block = int32_t(in_tile & ((1 << blocks_log2) - 1));
+    if (u != blockIdx.x || (!FEW && alone)) s = a.splits[in_tile >> blocks_log2];
+    const int32_t row = alone ? block : block * SIDE + side;
     const int32_t in_req = s.tile * a.rows + row;
     const int64_t step = int64_t(a.n_kv) * a.rows, at = (int64_t(s.part0) * a.n_kv + kvh) * a.rows + row;
-    if (in_req >= s.n_new * a.group) continue;  // (FEW: the whole workgroup)
+    if (in_req >= s.n_new * a.group) continue;  // (alone: the whole workgroup)
     const f32x2 *ml = a.parts.ml + at;
     const float *parts = a.parts.acc + at * D + sub * 4;
     float m = -INFINITY;
-    // (few rows: a side's first part is asked for with the maxima)
-    const bool has = FEW && side < s.n_parts;
+    // (alone: a side's first part is asked for with the maxima)
+    const bool has = alone && side < s.n_parts;
     const f32x2 ml0 = has ? ml[side * step] : f32x2{-INFINITY, 0.0f};
     const f32x4 v0 = has ? *reinterpret_cast<const f32x4 *>(parts + side * step * D) : f32x4{0, 0, 0, 0};
-    if (FEW) {
+    if (alone) {
       for (int32_t p = threadIdx.x & 63; p < s.n_parts; p += 64) m = fmaxf(m, ml[p * step].x);
 #pragma unroll
       for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i, 64));
@@ -282,7 +316,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
       acc = f32x4{w * v0[0], w * v0[1], w * v0[2], w * v0[3]};
     }
 #pragma unroll 4
-    for (int32_t p = FEW ? side + SIDE : 0; p < s.n_parts; p += FEW ? SIDE : 1) {
+    for (int32_t p = alone ? side + SIDE : 0; p < s.n_parts; p += alone ? SIDE : 1) {
       const f32x2 x = ml[p * step];
       const f32x4 v = *reinterpret_cast<const f32x4 *>(parts + p * step * D);
       const float w = exp2f(x.x - ms);
@@ -290,7 +324,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] = fmaf(w, v[i], acc[i]);
     }
-    if (FEW) {
+    if (alone) {
       sh[threadIdx.x] = acc;
       if (sub == 0) shl[side] = l;
       __syncthreads();
@@ -302,8 +336,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
         }
       }
     }
-    if (!FEW || side == 0) write_row<T, D, FEW>(a, s, in_req, kvh, sub, acc, m, l);
-    if (FEW) __syncthreads();
+    if (!alone || side == 0) write_row<T, D, FEW>(a, s, in_req, kvh, sub, acc, m, l);
+    if (alone) __syncthreads();
   }
 }
 
