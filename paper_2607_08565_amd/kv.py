@@ -12,6 +12,7 @@ theirs; there is no CPU fallback.
 """
 from __future__ import annotations
 
+import collections
 import ctypes as C
 
 import torch
@@ -28,18 +29,28 @@ _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2, _E2M1: 3
 GROUP = 32  # components of a 4-bit cache with one exponent
 
 
+class _Kept:
+    """What the library is given by address: the last few of them stay, so that the address of one
+    that was made for a single call is good for that call."""
+    _last: collections.deque = collections.deque(maxlen=64)
+
+    def __init__(self, *fields, **named):
+        super().__init__(*fields, **named)
+        self._last.append(self)
+
+
 class _Exps(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3)]
 
 
-class _Cache(C.Structure):
+class _Cache(_Kept, C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("k_stride", C.c_int64 * 3),
                 ("v_stride", C.c_int64 * 3), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("exps", C.c_void_p)]
 
 
-class _Rotary(C.Structure):
+class _Rotary(_Kept, C.Structure):
     _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("table", C.c_void_p), ("n_pos", C.c_int64),
                 ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float)]
 

@@ -138,6 +138,17 @@ def test_binding_refuses_caps():
                 kv.attend(e(torch.bfloat16, 0, 4, 64), c, e(torch.int32, 0, 4), plan, cap=cap)
 
 
+def test_addresses_of_a_call_stay_good():
+    """A structure made for one call and dropped is still what its address shows, after much else was made."""
+    at = [C.addressof(kv._Cache(FAKE + 16 * i, FAKE, 7, strides(1, 2, 3), strides(4, 5, 6), 16, 2, 64, 0, None, None)) for i in range(20)]
+    at.append(C.addressof(kv._Rotary(FAKE, FAKE, FAKE, 9, 64, 0, 1e-6)))
+    other = [bytes(112) for _ in range(1000)] + [bytearray(104) for _ in range(1000)]
+    for i, a in enumerate(at[:20]):
+        c = kv._Cache.from_address(a)
+        assert (c.k, c.v, c.n_pages, list(c.v_stride), c.head_dim) == (FAKE + 16 * i, FAKE, 7, [4, 5, 6], 64)
+    assert kv._Rotary.from_address(at[20]).n_pos == 9 and len(other) == 2000
+
+
 def test_plain_form_of_the_codes():
     """The reference against the levels' own table: every midpoint goes to the even code, k is smallest."""
     lv = ref4.LEVELS
