@@ -155,11 +155,11 @@ int smetric_kv_read(int32_t dtype, const smetric_kv_cache *cache /* host */, con
  *   s_j = scale (q . k_j),  out = sum_j exp(s_j - lse) v_j,  lse = log(sum_j exp(s_j))
  * and out = 0, lse = -inf when it sees nothing.  Scores, maxima, sums and the output are
  * held in float32; exp(s_j - m), with m the largest score so far or at most log(2^8) below it, is
- * rounded to the activations' type for the product with the values (F16 loses bits of those below
- * 2^-21 of the largest, BF16 holds 8 of any).  What E2M1 pages hold is rounded to the activations' type
- * first: exact for what smetric_kv_append enters.  Tokens that a row does not see change not a bit of
- * it, whatever they hold; nor does what a page holds past kv_len.  Splits are joined in a fixed order, so the same call
- * gives the same bits.
+ * rounded to the activations' type for the product with the values and for the sum that this is divided
+ * by (F16 loses bits of those below 2^-21 of the largest, BF16 holds 8 of any), not for lse's.  What
+ * E2M1 pages hold is rounded to the activations' type first: exact for what smetric_kv_append enters.
+ * Tokens that a row does not see change not a bit of it, whatever they hold; nor does what a page holds
+ * past kv_len.  Splits are joined in a fixed order, so the same call gives the same bits.
  *
  * The plan holds how the batch's rows and cached tokens are split into pieces of work.  It
  * depends on the lengths alone: one smetric_attend_plan per step serves every layer's

@@ -76,14 +76,14 @@ inline PlanShape plan_shape(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_
   s.off_splits = s.off_items + s.max_items * int64_t(sizeof(PlanItem));
   s.off_first = s.off_splits + s.max_splits * int64_t(sizeof(PlanSplit));
   s.plan_bytes = uint64_t(s.off_first + (s.max_groups + 1) * 4 + 255) / 256 * 256;
-  // per part, key-value head and row: the sums over its keys, then their maximum and weight
-  s.ws_bytes = uint64_t(s.max_parts) * n_kv * s.rows * (head_dim + 2) * 4;
+  // per part, key-value head and row: the sums over its keys, then their maximum and weights
+  s.ws_bytes = uint64_t(s.max_parts) * n_kv * s.rows * (head_dim + 4) * 4;
   return s;
 }
 
 struct PartView {
   float *acc;  // [part][kv head][row][head_dim]
-  f32x2 *ml;   // [part][kv head][row]: maximum (in powers of two), sum of weights
+  f32x4 *ml;   // [part][kv head][row]: maximum (in powers of two), sum of rounded weights, of unrounded ones (for lse)
 };
 struct AttendArgs {
   const PlanHdr *hdr;
@@ -219,7 +219,6 @@ __device__ __forceinline__ f32x4 four_values(const Place &p, int c) {
 
 // 16 lanes read four rows' 16 columns of 16-bit values from LDS, each lane's address a row's
 // (lane / 4) four columns (lane % 4): lane i gets column i of the four rows.
-typedef __attribute__((ext_vector_type(4))) short s16x4;
 __device__ __forceinline__ u32x2 read_transposed(const char *lds) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                        (__attribute__((address_space(3))) s16x4 *)lds));

@@ -13,6 +13,8 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -40,6 +42,15 @@ struct Bf16 {
   __device__ static __forceinline__ float hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
   __device__ static __forceinline__ uint32_t pack(float a, float b) {  // to nearest even, v_cvt_pk_bf16_f32
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
+  }
+  // Sums in float32 of packed weights as the products take them (checked: rounded as additions are):
+  // s and two of them; c (each of its components) and four
+  __device__ static __forceinline__ float add_two(uint32_t x, float s) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, 0x3F803F80u), s, false);
+  }
+  __device__ static __forceinline__ f32x4 add_four(u32x2 x, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, u32x2{0x3F803F80u, 0x3F803F80u}),
+                                                  __builtin_bit_cast(s16x4, x), c, 0, 0, 0);
   }
   // two of the four E4M3 values in x
   template <bool HIGH>
@@ -73,6 +84,13 @@ struct F16 {
   __device__ static __forceinline__ float hi(uint32_t x) { return float(__builtin_bit_cast(f16x2, x).y); }
   __device__ static __forceinline__ uint32_t pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2));
+  }
+  __device__ static __forceinline__ float add_two(uint32_t x, float s) {  // (subnormal ones as they are, as the products take them)
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, x), __builtin_bit_cast(f16x2, 0x3C003C00u), s, false);
+  }
+  __device__ static __forceinline__ f32x4 add_four(u32x2 x, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_4x4x4f16(__builtin_bit_cast(f16x4, u32x2{0x3C003C00u, 0x3C003C00u}),
+                                              __builtin_bit_cast(f16x4, x), c, 0, 0, 0);
   }
   template <bool HIGH>
   __device__ static __forceinline__ uint32_t from_e4m3(uint32_t x) {

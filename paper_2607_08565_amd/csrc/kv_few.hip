@@ -13,7 +13,8 @@
 // lane exchanges, and the weights are where the second product, O^T = V^T P^T, wants them:
 // its order of keys is free as long as both operands use one, so the order in which S^T
 // leaves them is used.  The next 32 keys' loads are in flight during all of it.  Weights are rounded
-// to the activations' type for it, as the matrix cores take 16-bit operands; their sum is not.
+// to the activations' type for it, as the matrix cores take 16-bit operands, and the output is divided by the sum
+// of rounded ones, so that equal values come out as they are; lse has the sum of unrounded ones.
 //
 // Measured: 32 requests decoding over 1.73 GB of cache 305 us, 5.7 TB/s (a copy of 4 GiB moves
 // 4.8); 64 drafted tokens over 0.58 GB 117 us; 131,072 keys of 8 bits (134 MB) 31 to 35 us, 24
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
   constexpr int SUMS = (16 * PADDED * 4 + 2 * D - 1) / (2 * D) * (2 * D), REGION = FK * 2 * D > SUMS ? FK * 2 * D : SUMS;
   constexpr int SWZ = D == 64 ? 3 : 7;
   __shared__ __attribute__((aligned(2 * D))) char lds[FW * REGION];
-  __shared__ float ml[FW][16][2];
+  __shared__ float ml[FW][16][3];  // maximum, sum of rounded weights, of unrounded ones
 
   const int32_t kvh = blockIdx.x % a.n_kv, share = blockIdx.x / a.n_kv;
   // asked for together: a workgroup's start is a chain of round trips
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
     f32x4 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, l = 0.0f, exact = 0.0f;
     bool odd = false;  // a value that rows see differently is not finite
     if (kb0 < k1) {
       if (WIDE) find_blocks(kb0);
@@ -308,6 +309,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
         const float down = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
         m = mn;
         l *= down;
+        exact *= down;
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] *= down;
       }
@@ -315,12 +317,14 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
 #pragma unroll
       for (int e = 0; e < 4 * NJ; ++e) {
         p[e] = __builtin_amdgcn_exp2f(LATE ? fmaf(p[e], sc, -base) : p[e] - base);
-        l += p[e];
+        exact += p[e];
       }
 #pragma unroll
       for (int t = 0; t < NJ / 2; ++t) {
         const u32x4 pw{T::pack(p[8 * t], p[8 * t + 1]), T::pack(p[8 * t + 2], p[8 * t + 3]), T::pack(p[8 * t + 4], p[8 * t + 5]),
                        T::pack(p[8 * t + 6], p[8 * t + 7])};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l = T::add_two(pw[e], l);
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
           const char *x = lds + (from_now ^ 32 * i) + t * 32 * (2 * D);
@@ -352,6 +356,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
 
     // join the wavefronts
     l = sum4(l);
+    exact = sum4(exact);
     wave_fence();
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -359,6 +364,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
     if (grp == 0) {
       ml[wave][col][0] = m;
       ml[wave][col][1] = l;
+      ml[wave][col][2] = exact;
     }
     __syncthreads();
     constexpr int N = D / 16;  // components of a thread
@@ -368,13 +374,14 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
 #pragma unroll
       for (int w = 1; w < FW; ++w) mm = fmaxf(mm, ml[w][jr][0]);
       const float ms = mm == -INFINITY ? 0.0f : mm;
-      float acc[N], ll = 0.0f;
+      float acc[N], ll = 0.0f, le = 0.0f;
 #pragma unroll
       for (int i = 0; i < N; ++i) acc[i] = 0.0f;
 #pragma unroll
       for (int w = 0; w < FW; ++w) {
         const float f = __builtin_amdgcn_exp2f(ml[w][jr][0] - ms);
         ll = fmaf(f, ml[w][jr][1], ll);
+        le = fmaf(f, ml[w][jr][2], le);
         const float *x = reinterpret_cast<const float *>(lds + w * REGION) + jr * PADDED + jc;
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[i] = fmaf(f, x[i], acc[i]);
@@ -388,14 +395,14 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
         for (int i = 0; i < N; i += 4)
           *reinterpret_cast<u32x2 *>(p + i) =
               u32x2{T::pack(acc[i] * inv, acc[i + 1] * inv), T::pack(acc[i + 2] * inv, acc[i + 3] * inv)};
-        if (a.lse && jc == 0) a.lse[(int64_t(it.tok0) + jt) * a.n_q + jh] = lse_of(mm, ll, T::FEW_SHIFT);
+        if (a.lse && jc == 0) a.lse[(int64_t(it.tok0) + jt) * a.n_q + jh] = lse_of(mm, le, T::FEW_SHIFT);
       } else {
         const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * FEW_ROWS + jr;
 #pragma unroll
         for (int i = 0; i < N; i += 4)
           *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + jc + i) =
               f32x4{acc[i] * vs, acc[i + 1] * vs, acc[i + 2] * vs, acc[i + 3] * vs};
-        if (jc == 0) a.parts.ml[slot] = f32x2{mm, ll};
+        if (jc == 0) a.parts.ml[slot] = f32x4{mm, ll, le, 0.0f};
       }
     }
     __syncthreads();  // the next piece's values go where these sums were

@@ -12,8 +12,8 @@
 // The products are S^T = K Q^T and O^T = V^T P^T: a lane holds scores of one row only, so its
 // maximum takes one lane exchange, and its weights are where the second product wants them --
 // the order in which S^T leaves the keys is the order in which V^T is read, transposed, from LDS.
-// Weights are rounded to the activations' type for it, as the matrix cores take 16-bit operands;
-// their sum is not.
+// Weights are rounded to the activations' type for it, as the matrix cores take 16-bit operands, and
+// so are those that they are divided by the sum of (WeightSum); lse has the sum of unrounded ones.
 //
 // Measured: 4,096 tokens over 16,384 (32 heads of 128) 923 to 986 us, 1,041 to 976 TFLOP/s, from card to card; on the
 // faster one the library's product of matrices of 16,384 reaches 1,402, of 8,192 1,173.  The matrix cores work half of the cycles
@@ -79,8 +79,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // one instr
 }
 
 // A row is scaled down only when its own maximum has grown by more than 2^SLACK: until then its
-// weights are at most 2^SLACK instead of 1, which costs BF16 no precision and F16 that many of the
-// powers of two below 1 (MANY_SHIFT), and most steps of a long request leave the sums alone.
+// weights are at most 2^SLACK instead of 1, and most steps of a long request leave the sums alone.  The
+// largest weight is then not 1, which rounding leaves as it is, but rounded as the others are (hence
+// WeightSum), and F16 has that many powers of two fewer below 1 (MANY_SHIFT).
 constexpr float SLACK = 8.0f;
 
 // Where a row's 16-byte pieces are in LDS: piece c at c ^ key_swap(row), c ^ value_swap(row).  A
@@ -112,12 +113,59 @@ __device__ __forceinline__ int flip_of(int row, int lane_col) {
 // cores take 32 cycles each for.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
+// What is done to a product before it is a score (smetric_attend_scores):
+//   BIASED  the bias, divided by the factor to come, is where the products' sums begin, instead of 0
+//   CAPPED  capped by so little that the weights need no running maximum, with BF16, whose weights have
+//           float32's range: scores are within cap of 0, and with m = min(cap, 84 - cap) in powers of
+//           two, cap up to 73 (50.5 natural), weights are between 2^-84 and 2^62: far from both ends
+//           also times values and summed over 2^24 keys.  That saves the maxima, a subtraction and the
+//           sums' scaling (2,048 tokens over 8,048: 195 us, without 175)
+//   OTHER   capped and, maybe, biased then
+// Capping takes five instructions a score, two of them at half rate, as long as the matrix cores take
+// for it at heads of 128: so the first 32 keys' scores are capped during the other 32's products, and
+// the others' (CAPPED) during those with the values (175 us, so 168).
+enum Scores { PLAIN, BIASED, CAPPED, OTHER };
+constexpr float CAPPED_MOST = 73.0f;
+__device__ __forceinline__ float capped_maximum(float cap) { return fminf(cap, 84.0f - cap); }
+
+// The sum of the weights that the products with the values take, rounded as they are: a sum of unrounded
+// ones leaves equal values other than they are, by up to the weights' half step.  (lse has the unrounded
+// ones' sum, 32 additions a step more.)  16 dot products with ones a step, each at half rate, or eight
+// matrix products of 8 cycles with a matrix of ones (4 x 4 x 4: a lane's own four), MATRIX: 4,096 tokens
+// over 16,384 with lse 1,005 us, with dot products 1,029, with a sum of unrounded ones 980; capped, whose
+// matrix cores wait less, 1,186 and 1,178; heads of 256, where registers are short, 309 and 298.
+template <int D, Scores S>
+struct WeightSum {
+  static constexpr bool MATRIX = D < 256 && S != CAPPED && S != OTHER;
+  std::conditional_t<MATRIX, f32x4, float> s;
+  __device__ __forceinline__ WeightSum() : s{} {}
+  // part i of n of 16 keys' 8 weights
+  template <typename T>
+  __device__ __forceinline__ void add(u32x4 p, int i, int n) {
+    if constexpr (MATRIX) {
+#pragma unroll
+      for (int e = 2 * i / n; e < 2 * (i + 1) / n; ++e) s = T::add_four(u32x2{p[2 * e], p[2 * e + 1]}, s);
+    } else {
+#pragma unroll
+      for (int e = 4 * i / n; e < 4 * (i + 1) / n; ++e) s = T::add_two(p[e], s);
+    }
+  }
+  __device__ __forceinline__ float get() const {
+    if constexpr (MATRIX)
+      return s.x;
+    else
+      return s;
+  }
+};
+
 // What a wavefront keeps of its 32 rows; lane (half, col) holds row col's.
-template <int D>
+template <int D, Scores S>
 struct Rows {
   u32x4 q[D / 16];
   f32x16 o[D / 32];  // O^T: components 32 i + 8 (r / 4) + 4 half + r % 4
-  float m, l;        // of the half's keys (l), of all (m)
+  float m;           // maximum
+  WeightSum<D, S> l; // of the half's keys: weights as the products take them, rounded
+  float exact;       // the same unrounded (LSE)
   int32_t hi, lo;    // the keys [lo, hi) that the row sees
   float slope;       // other scores: a key's bias by distance, of the products' sums or in powers of two
 };
@@ -144,26 +192,11 @@ struct Values {
   }
 };
 
-// What is done to a product before it is a score (smetric_attend_scores):
-//   BIASED  the bias, divided by the factor to come, is where the products' sums begin, instead of 0
-//   CAPPED  capped by so little that the weights need no running maximum, with BF16, whose weights have
-//           float32's range: scores are within cap of 0, and with m = min(cap, 84 - cap) in powers of
-//           two, cap up to 73 (50.5 natural), weights are between 2^-84 and 2^62: far from both ends
-//           also times values and summed over 2^24 keys.  That saves the maxima, a subtraction and the
-//           sums' scaling (2,048 tokens over 8,048: 195 us, without 175)
-//   OTHER   capped and, maybe, biased then
-// Capping takes five instructions a score, two of them at half rate, as long as the matrix cores take
-// for it at heads of 128: so the first 32 keys' scores are capped during the other 32's products, and
-// the others' (CAPPED) during those with the values (175 us, so 168).
-enum Scores { PLAIN, BIASED, CAPPED, OTHER };
-constexpr float CAPPED_MOST = 73.0f;
-__device__ __forceinline__ float capped_maximum(float cap) { return fminf(cap, 84.0f - cap); }
-
 // One step's 64 keys: the scores.  S^T: lane (half, col) gets row col's scores of keys kb +
 // 32 j + 8 (r / 4) + 4 half + r % 4, -inf for those that the row does not see (MASKED: there
 // may be some).  Returns the row's largest, and the first 16 keys' values on their way.
 template <typename T, int D, bool MASKED, Scores S>
-__device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, const char *kl, const char *vl, int32_t kb,
+__device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D, S> &w, const char *kl, const char *vl, int32_t kb,
                                         float sc, int lane, f32x16 (&s)[2], Values<D> &first) {
   constexpr int N = D / 8, AHEAD = 4, ROWB = 2 * D;
   constexpr bool CAP = S == CAPPED || S == OTHER;
@@ -234,17 +267,18 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D> &w, c
   const u32x2 both = swap32(__float_as_uint(mx), __float_as_uint(mx));
   return __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * (S == OTHER ? 1.0f : sc);
 }
-template <typename T, int D>
-__device__ __forceinline__ float exponent(const Rows<D> &w) {  // of weight 2^MANY_SHIFT
+template <typename T, int D, Scores S>
+__device__ __forceinline__ float exponent(const Rows<D, S> &w) {  // of weight 2^MANY_SHIFT
   return T::MANY_SHIFT - (w.m == -INFINITY ? 0.0f : w.m);
 }
 
 // The products of 16 keys' weights with their values, among them the next 16's weights and reads.
 // Capped scores are the weights' exponents, the last 32 keys' (LATER) after capping, which is done here.
-template <typename T, bool CAP, bool LATER, int D>
-__device__ __forceinline__ void products(const AttendArgs &a, Rows<D> &w, const char *vl, float sc, int lane,
+template <typename T, bool LATER, bool LSE, int D, Scores S>
+__device__ __forceinline__ void products(const AttendArgs &a, Rows<D, S> &w, const char *vl, float sc, int lane,
                                          const f32x16 (&s)[2], const Values<D> &first) {
   constexpr int DT = D / 32;
+  constexpr bool CAP = S == CAPPED;
   const float base = exponent<T>(w);
   const Capped capped(a, sc, CAP ? capped_maximum(a.cap_log2) : 0.0f);
   const int off = Values<D>::offset(again(lane));
@@ -256,7 +290,7 @@ __device__ __forceinline__ void products(const AttendArgs &a, Rows<D> &w, const 
       return __builtin_amdgcn_exp2f(!CAP ? fmaf(z, sc, base) : LATER && t >= 2 ? capped(z) : z);
     };
     const float x = weight(s[t / 2][8 * (t % 2) + 2 * e]), y = weight(s[t / 2][8 * (t % 2) + 2 * e + 1]);
-    w.l += x + y;
+    if (LSE) w.exact += x + y;
     p[t % 2][e] = T::pack(x, y);
   };
 #pragma unroll
@@ -269,6 +303,7 @@ __device__ __forceinline__ void products(const AttendArgs &a, Rows<D> &w, const 
       if (t == 0 && i == 0) __builtin_amdgcn_s_setprio(1);
       const Values<D> &x = v[t % 2];
       w.o[i] = T::mfma32(u32x4{x.lo[i].x, x.lo[i].y, x.hi[i].x, x.hi[i].y}, p[t % 2], w.o[i]);
+      w.l.template add<T>(p[t % 2], i, DT);
       if (t + 1 < KT / 16) {
         v[(t + 1) % 2].read(vl, off, t + 1, i);
 #pragma unroll
@@ -308,8 +343,8 @@ __device__ __forceinline__ void scale_down(f32x16 &o, float down, uint64_t grown
 }
 
 // A step.  ENDS: not every row sees all of its keys.
-template <typename T, int D, bool ENDS, Scores S>
-__device__ __forceinline__ void step(const AttendArgs &a, Rows<D> &w, const char *kl, const char *vl, int32_t kb, float sc,
+template <typename T, int D, bool ENDS, Scores S, bool LSE>
+__device__ __forceinline__ void step(const AttendArgs &a, Rows<D, S> &w, const char *kl, const char *vl, int32_t kb, float sc,
                                      int lane) {
   f32x16 s[2];
   Values<D> first;
@@ -321,24 +356,25 @@ __device__ __forceinline__ void step(const AttendArgs &a, Rows<D> &w, const char
       const bool mine = mx > w.m + SLACK;
       down = mine ? __builtin_amdgcn_exp2f(w.m - mx) : 1.0f;
       w.m = mine ? mx : w.m;
-      w.l *= down;
+      w.l.s *= down;
+      w.exact *= down;
     }
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
   }
-  products<T, S == CAPPED, !ENDS>(a, w, vl, S == OTHER ? 1.0f : sc, lane, s, first);
+  products<T, !ENDS, LSE>(a, w, vl, S == OTHER ? 1.0f : sc, lane, s, first);
 }
 
-// A wavefront's rows: the output, or the sums for the joining.
-template <typename T, int D>
-__device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &it, const Rows<D> &w, int32_t kvh, int wave,
-                                           int lane, float vs) {
+// A wavefront's rows: the output, or the sums for the joining.  l, exact: of both halves' keys.
+template <typename T, bool LSE, int D, Scores S>
+__device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &it, const Rows<D, S> &w, float l, float exact,
+                                           int32_t kvh, int wave, int lane, float vs) {
   constexpr int DT = D / 32;
   const int col = lane & 31, half = lane >> 5;
   const int32_t row = it.tile * MANY_ROWS + 32 * wave + col, tok = row / a.group, head = kvh * a.group + row % a.group;
   const bool has_row = row < it.n_new * a.group;
   if (it.part < 0) {
-    const float inv = w.l == 0.0f ? 0.0f : vs / w.l;
+    const float inv = l == 0.0f ? 0.0f : vs / l;
     uint16_t *p = a.out.data + (int64_t(it.tok0) + tok) * a.out.token + head * a.out.head;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -354,7 +390,7 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
         }
         if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
       }
-    if (a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of(w.m, w.l, T::MANY_SHIFT);
+    if (LSE && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of(w.m, exact, T::MANY_SHIFT);
   } else if (has_row) {
     const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
 #pragma unroll
@@ -363,7 +399,7 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
       for (int g = 0; g < 4; ++g)
         *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + 32 * i + 8 * g + 4 * half) =
             f32x4{w.o[i][4 * g] * vs, w.o[i][4 * g + 1] * vs, w.o[i][4 * g + 2] * vs, w.o[i][4 * g + 3] * vs};
-    if (half == 0) a.parts.ml[slot] = f32x2{w.m, w.l};
+    if (half == 0) a.parts.ml[slot] = f32x4{w.m, l, exact, 0.0f};
   }
 }
 
@@ -394,8 +430,8 @@ __device__ __forceinline__ void add_not_finite(const AttendArgs &a, const PlanIt
   }
 }
 
-// WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.
-template <typename T, Pages KV, int D, bool WIDE, Scores S>
+// WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.  LSE: it is asked for.
+template <typename T, Pages KV, int D, bool WIDE, Scores S, bool LSE>
 __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
   constexpr bool KV8 = KV == PAGES8, KV4 = KV == PAGES4;
   constexpr int PB = KV4 ? piece4(D) : 16;  // bytes of a lane's load
@@ -430,7 +466,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     const int32_t k0 = uniform(too_long ? 0 : it.k0), k1 = uniform(too_long ? 0 : it.k1);
     if (too_long && threadIdx.x == 0) set_status(a.status, SMETRIC_EINVAL);
 
-    Rows<D> w;
+    Rows<D, S> w;
     const bool has_row = col < n_rows;
     const int32_t row = row0 + col, tok = row / a.group, head = kvh * a.group + row % a.group;
     const int32_t first = it.kv_len - it.n_new;  // the first new token's place
@@ -480,7 +516,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) w.o[i][r] = 0.0f;
     w.m = S == CAPPED ? capped_maximum(a.cap_log2) : -INFINITY;
-    w.l = 0.0f;
+    w.exact = 0.0f;
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
 
     const int32_t kb0 = k0 / KT * KT, last_key = k1 - 1;
@@ -617,7 +653,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
         load_next(kb);
         if (ENDS) look_over(kb, here() + SIDE);
         if (!ENDS || (n_rows > 0 && kb < max_hi && kb + KT > min_lo))
-          step<T, D, ENDS, S>(a, w, here(), here() + SIDE, kb, sc, lane);
+          step<T, D, ENDS, S, LSE>(a, w, here(), here() + SIDE, kb, sc, lane);
         if (KV != PAGES16 && kb + KT < k1) to_16(there());
         arrived();
       }
@@ -638,12 +674,13 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
       }
     }
     if (bad_page) set_status(a.status, SMETRIC_EINVAL);
-    {
-      const u32x2 both = swap32(__float_as_uint(w.l), __float_as_uint(w.l));
-      w.l = __uint_as_float(both.x) + __uint_as_float(both.y);
-    }
+    const auto halves = [](float x) {
+      const u32x2 both = swap32(__float_as_uint(x), __float_as_uint(x));
+      return __uint_as_float(both.x) + __uint_as_float(both.y);
+    };
+    const float l = halves(w.l.get()), exact = LSE ? halves(w.exact) : 0.0f;
     const float vs = KV8 && a.cache.v_scale ? a.cache.v_scale[kvh] : 1.0f;
-    write_rows<T>(a, it, w, kvh, wave, again(lane), vs);
+    write_rows<T, LSE>(a, it, w, l, exact, kvh, wave, again(lane), vs);
     if (kb0 < k1 && odd_piece == piece) {  // (the next piece's first barrier comes after all have read it)
 #pragma unroll 1
       for (int32_t key = k0; key < k1; ++key) {
@@ -660,10 +697,9 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
 template <typename T, Pages KV, int D, Scores S>
 int launch_s(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
   const dim3 grid(uint32_t(max_groups * a.n_kv)), block(MT);
-  if (a.cache.ps.size % 16 == 0)
-    many_kernel<T, KV, D, true, S><<<grid, block, 0, stream>>>(a);
-  else
-    many_kernel<T, KV, D, false, S><<<grid, block, 0, stream>>>(a);
+  const auto kernel = a.cache.ps.size % 16 == 0 ? a.lse ? many_kernel<T, KV, D, true, S, true> : many_kernel<T, KV, D, true, S, false>
+                                                : a.lse ? many_kernel<T, KV, D, false, S, true> : many_kernel<T, KV, D, false, S, false>;
+  kernel<<<grid, block, 0, stream>>>(a);
   return hip_status(hipGetLastError());
 }
 template <typename T, Pages KV, int D>

@@ -256,26 +256,26 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
 }
 
 // Joins the parts of a cut tile: out = sum_p 2^(m_p - m) acc_p / sum_p 2^(m_p - m) l_p, in the
-// order of the parts.  D / 4 threads hold a row.  Tiles of many rows: the workgroup takes as
+// order of the parts, l_p the sums of rounded weights (PartView); lse takes those of unrounded ones.  D / 4 threads hold a row.  Tiles of many rows: the workgroup takes as
 // many rows at once (each of a few parts).  Tiles of few rows, which may have hundreds of
 // parts, and of many where a few long requests share all of the parts: it takes one row's parts
 // side by side (2 requests of 7 new tokens over 47,760, 14 heads on 2: 44 us, so 7).
 constexpr int32_t JOIN_GRID = 2048;
 template <typename T, int D, bool FEW>
 __device__ __forceinline__ void write_row(const AttendArgs &a, const PlanSplit &s, int32_t in_req, int32_t kvh, int sub,
-                                          f32x4 acc, float m, float l) {
+                                          f32x4 acc, float m, float l, float exact) {
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int64_t t = int64_t(s.tok0) + in_req / a.group;
   const int32_t head = kvh * a.group + in_req % a.group;
   *reinterpret_cast<u32x2 *>(a.out.data + t * a.out.token + head * a.out.head + sub * 4) =
       u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
-  if (a.lse && sub == 0) a.lse[t * a.n_q + head] = lse_of(m, l, FEW ? T::FEW_SHIFT : T::MANY_SHIFT);
+  if (a.lse && sub == 0) a.lse[t * a.n_q + head] = lse_of(m, exact, FEW ? T::FEW_SHIFT : T::MANY_SHIFT);
 }
 template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
   constexpr int TPP = D / 4, SIDE = 256 / TPP, BLOCKS = FEW ? FEW_ROWS : MANY_ROWS / SIDE;
   __shared__ f32x4 sh[256];
-  __shared__ float shl[SIDE];
+  __shared__ f32x2 shl[SIDE];
   // a short request's joining is a chain of round trips: the first unit's split is asked for with the header
   PlanSplit s = a.splits[blockIdx.x / a.n_kv / BLOCKS];
   const PlanHdr h = *a.hdr;
@@ -293,12 +293,12 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     const int32_t in_req = s.tile * a.rows + row;
     const int64_t step = int64_t(a.n_kv) * a.rows, at = (int64_t(s.part0) * a.n_kv + kvh) * a.rows + row;
     if (in_req >= s.n_new * a.group) continue;  // (alone: the whole workgroup)
-    const f32x2 *ml = a.parts.ml + at;
+    const f32x4 *ml = a.parts.ml + at;
     const float *parts = a.parts.acc + at * D + sub * 4;
     float m = -INFINITY;
     // (alone: a side's first part is asked for with the maxima)
     const bool has = alone && side < s.n_parts;
-    const f32x2 ml0 = has ? ml[side * step] : f32x2{-INFINITY, 0.0f};
+    const f32x4 ml0 = has ? ml[side * step] : f32x4{-INFINITY, 0.0f, 0.0f, 0.0f};
     const f32x4 v0 = has ? *reinterpret_cast<const f32x4 *>(parts + side * step * D) : f32x4{0, 0, 0, 0};
     if (alone) {
       for (int32_t p = threadIdx.x & 63; p < s.n_parts; p += 64) m = fmaxf(m, ml[p * step].x);
@@ -309,34 +309,37 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     }
     const float ms = m == -INFINITY ? 0.0f : m;
     f32x4 acc{0, 0, 0, 0};
-    float l = 0.0f;
+    float l = 0.0f, exact = 0.0f;
     if (has) {
       const float w = exp2f(ml0.x - ms);
       l = w * ml0.y;
+      exact = w * ml0.z;
       acc = f32x4{w * v0[0], w * v0[1], w * v0[2], w * v0[3]};
     }
 #pragma unroll 4
     for (int32_t p = alone ? side + SIDE : 0; p < s.n_parts; p += alone ? SIDE : 1) {
-      const f32x2 x = ml[p * step];
+      const f32x4 x = ml[p * step];
       const f32x4 v = *reinterpret_cast<const f32x4 *>(parts + p * step * D);
       const float w = exp2f(x.x - ms);
       l = fmaf(w, x.y, l);
+      exact = fmaf(w, x.z, exact);
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] = fmaf(w, v[i], acc[i]);
     }
     if (alone) {
       sh[threadIdx.x] = acc;
-      if (sub == 0) shl[side] = l;
+      if (sub == 0) shl[side] = f32x2{l, exact};
       __syncthreads();
       if (side == 0) {
 #pragma unroll
         for (int i = 1; i < SIDE; ++i) {
           acc += sh[i * TPP + sub];
-          l += shl[i];
+          l += shl[i].x;
+          exact += shl[i].y;
         }
       }
     }
-    if (!alone || side == 0) write_row<T, D, FEW>(a, s, in_req, kvh, sub, acc, m, l);
+    if (!alone || side == 0) write_row<T, D, FEW>(a, s, in_req, kvh, sub, acc, m, l, exact);
     if (alone) __syncthreads();
   }
 }
@@ -435,7 +438,7 @@ extern "C" int smetric_attend_scores(int32_t dtype, const smetric_kv_cache *cach
   a.lse = lse;
   const int64_t part_rows = s.max_parts * cache->n_kv_heads * s.rows;
   a.parts.acc = static_cast<float *>(workspace);
-  a.parts.ml = reinterpret_cast<f32x2 *>(a.parts.acc + part_rows * cache->head_dim);
+  a.parts.ml = reinterpret_cast<f32x4 *>(a.parts.acc + part_rows * cache->head_dim);
   a.n_tokens = batch->n_tokens;
   a.n_req = batch->n_req;
   a.n_q = n_q_heads;
