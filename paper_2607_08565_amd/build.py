@@ -14,7 +14,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsmetric.so")
 CALLS = os.path.join(HERE, "_kv_calls.so")
 SOURCES = ["hash.hip", "probe.hip", "match.hip", "route.hip", "index.hip", "session.hip", "metrics.hip", "score.hip",
-           "kv_rotate.hip", "kv_read.hip", "kv_plan.hip", "kv_few.hip", "kv_many.hip", "kv_few_scores.hip", "kv_many_scores.hip"]
+           "kv_rotate.hip", "kv_read.hip", "kv_plan.hip", "kv_few.hip", "kv_many.hip", "kv_few_scores.hip", "kv_many_scores.hip",
+           "kv_many_scores_f16.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

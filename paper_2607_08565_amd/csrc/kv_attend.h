@@ -117,7 +117,16 @@ __device__ __forceinline__ float lse_of(float m, float l, float shift) {
 int launch_few(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
 int launch_many(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
 int launch_few_scores(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
-int launch_many_scores(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+template <typename T>  // (a file each)
+int launch_many_scored(const AttendArgs &a, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+template <>
+int launch_many_scored<Bf16>(const AttendArgs &a, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+template <>
+int launch_many_scored<F16>(const AttendArgs &a, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream);
+inline int launch_many_scores(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
+  return dtype == SMETRIC_BF16 ? launch_many_scored<Bf16>(a, pages, head_dim, max_groups, stream)
+                               : launch_many_scored<F16>(a, pages, head_dim, max_groups, stream);
+}
 
 // Where a place's keys and values are in memory, and the exponents of E2M1 pages.
 struct Place {
@@ -169,18 +178,34 @@ __device__ __forceinline__ int again(int x) {
   return x;
 }
 
+// A factor of scores as float32 holds it: 0 times it is 0, NaN stays.
+__host__ __device__ __forceinline__ float finite_factor(float x) {
+  return x > 0x1.fffffep127f ? 0x1.fffffep127f : x < -0x1.fffffep127f ? -0x1.fffffep127f : x;
+}
+
 // Other scores (smetric_attend_scores), in powers of two: of x = q . k, sc = scale log2(e) (and the keys'
 // scale), the capped score, cap tanh(scale x / cap) = cap - 2 cap / (1 + exp(2 scale x / cap)): both ends
-// come out of the exponential's own overflow to infinity and underflow to zero.
+// come out of the exponential's own overflow to infinity and underflow to zero.  It loses some 2^-23 of
+// the cap, which a score of the cap's size does as well, and smaller ones of caps up to CAP_NEAR can
+// spare (2^-17).  Of larger caps scores below a quarter of it come from the series of tanh(u) = u (1 - u^2 / 3
+// + 2 u^4 / 15 - 17 u^6 / 315 + 62 u^8 / 2835), whose next term is below 2^-26: far().
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float CAP_NEAR = 64.0f * LOG2E;
 struct Capped {
   float rate, cap, top;  // of the exponent, 2 sc / cap; cap log2(e); that less m, which scores are taken from
-  __device__ __forceinline__ Capped(const AttendArgs &a, float sc, float m = 0.0f)
-      : rate(a.cap_log2 > 0.0f ? 2.8853900817779268f * sc / a.cap_log2 : 0.0f), cap(a.cap_log2), top(a.cap_log2 - m) {}
+  float sc, inverse;     // far(): 1 / (cap log2(e))
+  __device__ __forceinline__ Capped(const AttendArgs &a, float sc_, float m = 0.0f)
+      : rate(a.cap_log2 > 0.0f ? finite_factor(2.8853900817779268f * sc_ / a.cap_log2) : 0.0f), cap(a.cap_log2),
+        top(a.cap_log2 - m), sc(sc_), inverse(1.0f / a.cap_log2) {}
   __device__ __forceinline__ float operator()(float x) const {
     return fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * rate)), top);
   }
+  __device__ __forceinline__ float far(float x) const {  // (m: 0)
+    const float y = x * sc, u = y * inverse, z = u * u;
+    const float series = fmaf(z, fmaf(z, fmaf(z, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f);
+    return fabsf(u) < 0.25f ? fmaf(y, z * series, y) : (*this)(x);
+  }
 };
-constexpr float LOG2E = 1.4426950408889634f;
 
 // Whether one of eight 16-bit floats is infinite or NaN: its exponent is all ones, and adding
 // the exponent's lowest bit to the exponent alone carries into the (cleared) sign bit.

@@ -6,6 +6,7 @@
 // shape, strides and address from Python takes 0.6 us each, five of them in an append (8.6 us
 // a call through ctypes, where the kernel itself takes less than three).
 #include <Python.h>
+#include <math.h>
 
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -286,7 +287,8 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const smetric_batch batch = batch_of(d, a[4], a[5], a[6], tokens);
     const double scale = PyFloat_AsDouble(a[9]), cap = PyFloat_AsDouble(a[19]);
     if ((scale == -1.0 || cap == -1.0) && PyErr_Occurred()) throw Refused{};
-    const smetric_scores scores{float(cap), array<const float>(d, a[20], at::kFloat, "slopes")};
+    // (a cap that float32 holds as 0 is not none)
+    const smetric_scores scores{cap != 0.0 && float(cap) == 0.0f ? NAN : float(cap), array<const float>(d, a[20], at::kFloat, "slopes")};
     if (a[20] != Py_None && THPVariable_Unpack(a[20]).numel() != n_q)
       refuse(PyExc_ValueError, "%s: expected one per query head", "slopes");
     const int32_t max_new = whole32(a[10]), window = whole32(a[11]);

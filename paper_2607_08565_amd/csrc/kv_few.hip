@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
         q[s] = *reinterpret_cast<const u32x4 *>(a.q.data + (int64_t(it.tok0) + tok) * a.q.token + head * a.q.head + d);
     }
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
-    const float sc = a.scale_log2 * (KV8 && a.cache.k_scale ? a.cache.k_scale[kvh] : 1.0f);
+    const float sc = KV8 && a.cache.k_scale ? finite_factor(a.scale_log2 * a.cache.k_scale[kvh]) : a.scale_log2;
     const Capped capped(a, sc);
     const float slope = SCORES && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
     char *my = lds + wave * REGION;
@@ -281,7 +281,10 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
       float p[4 * NJ];
 #pragma unroll
       for (int e = 0; e < 4 * NJ; ++e) p[e] = s[e / 4][e % 4];
-      if (SCORES && capped.cap > 0.0f) {
+      if (SCORES && capped.cap > CAP_NEAR) {
+#pragma unroll
+        for (int e = 0; e < 4 * NJ; ++e) p[e] = capped.far(p[e]);
+      } else if (SCORES && capped.cap > 0.0f) {
 #pragma unroll
         for (int e = 0; e < 4 * NJ; ++e) p[e] = capped(p[e]);
       } else if (!LATE) {

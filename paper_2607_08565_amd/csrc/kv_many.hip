@@ -120,11 +120,13 @@ __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); 
 //           two, cap up to 73 (50.5 natural), weights are between 2^-84 and 2^62: far from both ends
 //           also times values and summed over 2^24 keys.  That saves the maxima, a subtraction and the
 //           sums' scaling (2,048 tokens over 8,048: 195 us, without 175)
-//   OTHER   capped and, maybe, biased then
+//   OTHER   capped and, maybe, biased then; FAR: caps above CAP_NEAR
 // Capping takes five instructions a score, two of them at half rate, as long as the matrix cores take
 // for it at heads of 128: so the first 32 keys' scores are capped during the other 32's products, and
 // the others' (CAPPED) during those with the values (175 us, so 168).
-enum Scores { PLAIN, BIASED, CAPPED, OTHER };
+enum Scores { PLAIN, BIASED, CAPPED, OTHER, FAR };
+constexpr bool caps(Scores s) { return s >= CAPPED; }
+constexpr bool caps_first(Scores s) { return s >= OTHER; }  // before a maximum is taken
 constexpr float CAPPED_MOST = 73.0f;
 __device__ __forceinline__ float capped_maximum(float cap) { return fminf(cap, 84.0f - cap); }
 
@@ -136,7 +138,7 @@ __device__ __forceinline__ float capped_maximum(float cap) { return fminf(cap, 8
 // matrix cores wait less, 1,186 and 1,178; heads of 256, where registers are short, 309 and 298.
 template <int D, Scores S>
 struct WeightSum {
-  static constexpr bool MATRIX = D < 256 && S != CAPPED && S != OTHER;
+  static constexpr bool MATRIX = D < 256 && !caps(S);
   std::conditional_t<MATRIX, f32x4, float> s;
   __device__ __forceinline__ WeightSum() : s{} {}
   // part i of n of 16 keys' 8 weights
@@ -199,7 +201,7 @@ template <typename T, int D, bool MASKED, Scores S>
 __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D, S> &w, const char *kl, const char *vl, int32_t kb,
                                         float sc, int lane, f32x16 (&s)[2], Values<D> &first) {
   constexpr int N = D / 8, AHEAD = 4, ROWB = 2 * D;
-  constexpr bool CAP = S == CAPPED || S == OTHER;
+  constexpr bool CAP = caps(S);
   const int l = again(lane), col = l & 31, swap = 16 * ((l >> 5) ^ key_swap<D>(col));
   const char *row = kl + col * ROWB;
   const auto piece = [&](int n) {  // (32 rows on: the same exchange)
@@ -209,12 +211,13 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D, S> &w
   u32x4 k[AHEAD];
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n) k[n] = piece(n);
-  const float from = S == BIASED || S == OTHER ? w.slope * float(kb + 4 * (lane >> 5) - (w.hi - 1)) : 0.0f;
+  const float from = S == BIASED || caps_first(S) ? w.slope * float(kb + 4 * (lane >> 5) - (w.hi - 1)) : 0.0f;
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[j][r] = S == BIASED ? fmaf(w.slope, float(32 * j + 8 * (r / 4) + r % 4), from) : 0.0f;
-  const Capped capped(a, sc, S == CAPPED ? capped_maximum(a.cap_log2) : 0.0f);
+  const Capped cap(a, sc, S == CAPPED ? capped_maximum(a.cap_log2) : 0.0f);
+  const auto capped = [&](float x) { return S == FAR ? cap.far(x) : cap(x); };
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     in_order();
@@ -236,11 +239,11 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D, S> &w
   if (CAP) {
 #pragma unroll
     for (int r = 16 - 32 / N; r < 16; ++r) s[0][r] = capped(s[0][r]);
-    if (S == OTHER || MASKED)  // (the others' among the products with the values: products)
+    if (caps_first(S) || MASKED)  // (the others' among the products with the values: products)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[1][r] = capped(s[1][r]);
   }
-  if (S == OTHER && a.slopes) {
+  if (caps_first(S) && a.slopes) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -265,7 +268,7 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D, S> &w
   for (int r = 1; r < 15; r += 2) mx = max3(mx, s[1][r], s[1][r + 1]);
   mx = __builtin_elementwise_maximum(mx, s[1][15]);
   const u32x2 both = swap32(__float_as_uint(mx), __float_as_uint(mx));
-  return __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * (S == OTHER ? 1.0f : sc);
+  return __builtin_elementwise_maximum(__uint_as_float(both.x), __uint_as_float(both.y)) * (caps_first(S) ? 1.0f : sc);
 }
 template <typename T, int D, Scores S>
 __device__ __forceinline__ float exponent(const Rows<D, S> &w) {  // of weight 2^MANY_SHIFT
@@ -362,7 +365,7 @@ __device__ __forceinline__ void step(const AttendArgs &a, Rows<D, S> &w, const c
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) scale_down(w.o[i], down, grown);
   }
-  products<T, !ENDS, LSE>(a, w, vl, S == OTHER ? 1.0f : sc, lane, s, first);
+  products<T, !ENDS, LSE>(a, w, vl, caps_first(S) ? 1.0f : sc, lane, s, first);
 }
 
 // A wavefront's rows: the output, or the sums for the joining.  l, exact: of both halves' keys.
@@ -390,7 +393,7 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
         }
         if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
       }
-    if (LSE && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of(w.m, exact, T::MANY_SHIFT);
+    if (LSE && a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of(w.m, exact, T::MANY_SHIFT);
   } else if (has_row) {
     const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
 #pragma unroll
@@ -487,7 +490,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     float sc = a.scale_log2;
     uint32_t flip = 0, nan = 0;
     if (KV8 && a.cache.k_scale) {
-      sc *= a.cache.k_scale[kvh];
+      sc = finite_factor(sc * a.cache.k_scale[kvh]);
       if (!(sc > 0.0f)) {
         flip = sc < 0.0f ? 0x80008000u : 0;
         nan = sc != sc ? 0x7FFF7FFFu : 0;
@@ -498,7 +501,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     // 2^66 of the queries (F16's become zeros: their scores are below 2^-20).
     const float smaller = S == BIASED && sc < 0x1p-60f ? 0x1p-66f : 1.0f;
     sc /= smaller;
-    w.slope = (S == BIASED || S == OTHER) && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
+    w.slope = (S == BIASED || caps_first(S)) && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
     if (S == BIASED) w.slope /= sc;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
@@ -697,8 +700,10 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
 template <typename T, Pages KV, int D, Scores S>
 int launch_s(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
   const dim3 grid(uint32_t(max_groups * a.n_kv)), block(MT);
-  const auto kernel = a.cache.ps.size % 16 == 0 ? a.lse ? many_kernel<T, KV, D, true, S, true> : many_kernel<T, KV, D, true, S, false>
-                                                : a.lse ? many_kernel<T, KV, D, false, S, true> : many_kernel<T, KV, D, false, S, false>;
+  constexpr bool ALONE = S == FAR;  // (rare: one form for both)
+  const bool lse = ALONE || a.lse;
+  const auto kernel = a.cache.ps.size % 16 == 0 ? lse ? many_kernel<T, KV, D, true, S, true> : many_kernel<T, KV, D, true, S, ALONE>
+                                                : lse ? many_kernel<T, KV, D, false, S, true> : many_kernel<T, KV, D, false, S, ALONE>;
   kernel<<<grid, block, 0, stream>>>(a);
   return hip_status(hipGetLastError());
 }
@@ -708,6 +713,7 @@ int launch_d(const AttendArgs &a, int64_t max_groups, hipStream_t stream) {
   if constexpr (std::is_same_v<T, Bf16>)
     if (!a.slopes && a.cap_log2 <= CAPPED_MOST) return launch_s<T, KV, D, CAPPED>(a, max_groups, stream);
   if (!(a.cap_log2 > 0.0f)) return launch_s<T, KV, D, BIASED>(a, max_groups, stream);
+  if (a.cap_log2 > CAP_NEAR) return launch_s<T, KV, D, FAR>(a, max_groups, stream);
   return launch_s<T, KV, D, OTHER>(a, max_groups, stream);
 #else
   return launch_s<T, KV, D, PLAIN>(a, max_groups, stream);
@@ -728,13 +734,15 @@ int launch_t(const AttendArgs &a, Pages p, int32_t d, int64_t max_groups, hipStr
 }  // namespace
 
 #ifdef SCORED
-int launch_many_scores(
+template <>
+int launch_many_scored<SCORED>(const AttendArgs &a, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
+  return launch_t<SCORED>(a, pages, head_dim, max_groups, stream);
+}
 #else
-int launch_many(
-#endif
-    const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
+int launch_many(const AttendArgs &a, int32_t dtype, Pages pages, int32_t head_dim, int64_t max_groups, hipStream_t stream) {
   return dtype == SMETRIC_BF16 ? launch_t<Bf16>(a, pages, head_dim, max_groups, stream)
                                : launch_t<F16>(a, pages, head_dim, max_groups, stream);
 }
+#endif
 
 }  // namespace smk

@@ -1,3 +1,3 @@
-// The kernels of kv_many.hip with scores that are capped or have a bias by distance, compiled apart.
-#define SCORED
+// Capped and biased scores' kernels of BF16, compiled beside the plain ones.
+#define SCORED Bf16
 #include "kv_many.hip"

@@ -365,7 +365,7 @@ int launch_join(const AttendArgs &a, int32_t head_dim, int64_t max_splits, hipSt
 // A window of all places is none: what the kernels subtract from a place stays in 32 bits.
 int32_t window_of(int32_t window) { return window >= MAX_PLACES ? 0 : window; }
 
-// Caps whose rates and products stay far from float32's ends.
+// Caps that stay far from float32's ends, as their squares do.
 constexpr float CAP_MIN = 0x1p-20f, CAP_MAX = 0x1p20f;
 
 bool shape_ok(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t max_new) {
@@ -447,7 +447,7 @@ extern "C" int smetric_attend_scores(int32_t dtype, const smetric_kv_cache *cach
   a.rows = s.rows;
   a.dim = cache->head_dim;
   a.window = window_of(window);
-  a.scale_log2 = scale * LOG2E;
+  a.scale_log2 = finite_factor(scale * LOG2E);
   a.cap_log2 = scores->cap * LOG2E;
   a.slopes = scores->slopes;
   a.status = status;
