@@ -193,7 +193,8 @@ int smetric_attend(int32_t dtype, const smetric_kv_cache *cache /* host */, cons
  *   cap     0: scores as they are; else a number in [2^-20, 2^20]
  *   slopes  float32[n_q_heads], of either sign, magnitudes up to 2^20, or NULL: no bias
  * Scores are float32's: capped ones are off by some 2^-23 cap of caps up to 64, of larger ones by some
- * 2^-21 of themselves, a bias by some 2^-22 of itself.  Caps up to
+ * 2^-21 of themselves, a bias by (head_dim / 16 + 8) 2^-24 of how far it is below the largest that the
+ * row sees.  Caps up to
  * 50.5 without slopes, BF16, chunks: weights are held times up to 2^62, so values up to 2^40 stay finite.
  * Host errors: smetric_attend's, and EINVAL for another cap. */
 typedef struct smetric_scores {

@@ -83,7 +83,7 @@ inline PlanShape plan_shape(int32_t n_req, int64_t n_tokens, int32_t n_q, int32_
 
 struct PartView {
   float *acc;  // [part][kv head][row][head_dim]
-  f32x4 *ml;   // [part][kv head][row]: maximum (in powers of two), sum of rounded weights, of unrounded ones (for lse)
+  f32x4 *ml;   // [part][kv head][row]: maximum (in powers of two), sum of rounded weights, of unrounded ones (for lse); what lse is more (Bias)
 };
 struct AttendArgs {
   const PlanHdr *hdr;
@@ -107,9 +107,9 @@ __device__ __forceinline__ bool plan_fits(const AttendArgs &a, const PlanHdr &h)
          h.dim == a.dim && h.window == a.window && h.n_tokens == a.n_tokens;
 }
 
-// lse from a row's maximum (in powers of two) and sum of weights times 2^shift.
-__device__ __forceinline__ float lse_of(float m, float l, float shift) {
-  return l == 0.0f ? -INFINITY : (m + log2f(l * exp2f(-shift))) * 0.693147180559945309f;
+// lse from a row's maximum (in powers of two) and sum of weights times 2^shift; more: Bias.
+__device__ __forceinline__ float lse_of(float m, float l, float shift, float more) {
+  return l == 0.0f ? -INFINITY : (m + log2f(l * exp2f(-shift)) + more) * 0.693147180559945309f;
 }
 
 // Launches (one per file; those of other scores apart).  Grids cover plan_shape's bounds;
@@ -205,6 +205,17 @@ struct Capped {
     const float series = fmaf(z, fmaf(z, fmaf(z, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f);
     return fabsf(u) < 0.25f ? fmaf(y, z * series, y) : (*this)(x);
   }
+};
+
+// A row's bias by distance, in powers of two: slope (key - place), taken less the largest that the row sees, at its
+// own place or, of slopes below zero, at its first key.  That leaves the output as it is, and the keys that count
+// most have a small one, of which float32 holds much: of 65,536 keys with a slope of -1/2 they would have 32,768.
+// What was taken off is added to lse.
+struct Bias {
+  float slope;
+  int32_t from;  // the key with a bias of 0
+  __device__ __forceinline__ Bias(float s, int32_t place, int32_t lo) : slope(s), from(s < 0.0f && lo > 0 ? lo : s < 0.0f ? 0 : place) {}
+  __device__ __forceinline__ float more(int32_t place) const { return slope * float(from - place); }
 };
 
 // Whether one of eight 16-bit floats is infinite or NaN: its exponent is all ones, and adding

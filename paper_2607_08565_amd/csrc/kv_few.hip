@@ -74,6 +74,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
   constexpr int SWZ = D == 64 ? 3 : 7;
   __shared__ __attribute__((aligned(2 * D))) char lds[FW * REGION];
   __shared__ float ml[FW][16][3];  // maximum, sum of rounded weights, of unrounded ones
+  __shared__ float more[SCORES ? 16 : 1];  // what lse is more
 
   const int32_t kvh = blockIdx.x % a.n_kv, share = blockIdx.x / a.n_kv;
   // asked for together: a workgroup's start is a chain of round trips
@@ -121,7 +122,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
     const float sc = KV8 && a.cache.k_scale ? finite_factor(a.scale_log2 * a.cache.k_scale[kvh]) : a.scale_log2;
     const Capped capped(a, sc);
-    const float slope = SCORES && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
+    const Bias bias(SCORES && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f, place, lo);
     char *my = lds + wave * REGION;
     // Where in LDS a lane's values go: 16-byte piece c of row r at c ^ 2 (r & SWZ), so that the transposed
     // reads, of eight rows' two pieces at a time, meet no bank twice.  What depends on the lane is
@@ -292,9 +293,9 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
         for (int e = 0; e < 4 * NJ; ++e) p[e] *= sc;
       }
       if (SCORES && a.slopes) {
-        const float from = slope * float(kb + 4 * grp - place);
+        const float from = bias.slope * float(kb + 4 * grp - bias.from);
 #pragma unroll
-        for (int e = 0; e < 4 * NJ; ++e) p[e] += fmaf(slope, float(16 * (e / 4) + e % 4), from);
+        for (int e = 0; e < 4 * NJ; ++e) p[e] += fmaf(bias.slope, float(16 * (e / 4) + e % 4), from);
       }
       if (masked) {
 #pragma unroll
@@ -368,6 +369,7 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
       ml[wave][col][0] = m;
       ml[wave][col][1] = l;
       ml[wave][col][2] = exact;
+      if (SCORES && wave == 0) more[col] = bias.more(place);
     }
     __syncthreads();
     constexpr int N = D / 16;  // components of a thread
@@ -398,14 +400,14 @@ __global__ __launch_bounds__(64 * few_waves(KV, D), at_once(D) * few_waves(KV, D
         for (int i = 0; i < N; i += 4)
           *reinterpret_cast<u32x2 *>(p + i) =
               u32x2{T::pack(acc[i] * inv, acc[i + 1] * inv), T::pack(acc[i + 2] * inv, acc[i + 3] * inv)};
-        if (a.lse && jc == 0) a.lse[(int64_t(it.tok0) + jt) * a.n_q + jh] = lse_of(mm, le, T::FEW_SHIFT);
+        if (a.lse && jc == 0) a.lse[(int64_t(it.tok0) + jt) * a.n_q + jh] = lse_of(mm, le, T::FEW_SHIFT, SCORES ? more[jr] : 0.0f);
       } else {
         const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * FEW_ROWS + jr;
 #pragma unroll
         for (int i = 0; i < N; i += 4)
           *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + jc + i) =
               f32x4{acc[i] * vs, acc[i + 1] * vs, acc[i + 2] * vs, acc[i + 3] * vs};
-        if (jc == 0) a.parts.ml[slot] = f32x4{mm, ll, le, 0.0f};
+        if (jc == 0) a.parts.ml[slot] = f32x4{mm, ll, le, SCORES ? more[jr] : 0.0f};
       }
     }
     __syncthreads();  // the next piece's values go where these sums were

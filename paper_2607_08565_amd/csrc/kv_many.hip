@@ -114,7 +114,8 @@ __device__ __forceinline__ int flip_of(int row, int lane_col) {
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // What is done to a product before it is a score (smetric_attend_scores):
-//   BIASED  the bias, divided by the factor to come, is where the products' sums begin, instead of 0
+//   BIASED  the bias, divided by the factor to come, is where the products' sums begin, instead of 0 (each of
+//           head_dim / 16 products rounds it, but of the keys that count it is small: Bias)
 //   CAPPED  capped by so little that the weights need no running maximum, with BF16, whose weights have
 //           float32's range: scores are within cap of 0, and with m = min(cap, 84 - cap) in powers of
 //           two, cap up to 73 (50.5 natural), weights are between 2^-84 and 2^62: far from both ends
@@ -170,6 +171,7 @@ struct Rows {
   float exact;       // the same unrounded (LSE)
   int32_t hi, lo;    // the keys [lo, hi) that the row sees
   float slope;       // other scores: a key's bias by distance, of the products' sums or in powers of two
+  int32_t from;      // the key with a bias of 0
 };
 
 // The values of 16 keys of a step, V^T as the matrix instruction takes it: read in the order in
@@ -211,7 +213,7 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D, S> &w
   u32x4 k[AHEAD];
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n) k[n] = piece(n);
-  const float from = S == BIASED || caps_first(S) ? w.slope * float(kb + 4 * (lane >> 5) - (w.hi - 1)) : 0.0f;
+  const float from = S == BIASED || caps_first(S) ? w.slope * float(kb + 4 * (lane >> 5) - w.from) : 0.0f;
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -371,7 +373,7 @@ __device__ __forceinline__ void step(const AttendArgs &a, Rows<D, S> &w, const c
 // A wavefront's rows: the output, or the sums for the joining.  l, exact: of both halves' keys.
 template <typename T, bool LSE, int D, Scores S>
 __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &it, const Rows<D, S> &w, float l, float exact,
-                                           int32_t kvh, int wave, int lane, float vs) {
+                                           float more, int32_t kvh, int wave, int lane, float vs) {
   constexpr int DT = D / 32;
   const int col = lane & 31, half = lane >> 5;
   const int32_t row = it.tile * MANY_ROWS + 32 * wave + col, tok = row / a.group, head = kvh * a.group + row % a.group;
@@ -393,7 +395,7 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
         }
         if (has_row) *reinterpret_cast<u32x4 *>(p + 32 * i + 8 * g + 8 * half) = x;
       }
-    if (LSE && a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of(w.m, exact, T::MANY_SHIFT);
+    if (LSE && a.lse && has_row && half == 0) a.lse[(int64_t(it.tok0) + tok) * a.n_q + head] = lse_of(w.m, exact, T::MANY_SHIFT, more);
   } else if (has_row) {
     const int64_t slot = (int64_t(it.part) * a.n_kv + kvh) * MANY_ROWS + 32 * wave + col;
 #pragma unroll
@@ -402,7 +404,7 @@ __device__ __forceinline__ void write_rows(const AttendArgs &a, const PlanItem &
       for (int g = 0; g < 4; ++g)
         *reinterpret_cast<f32x4 *>(a.parts.acc + slot * D + 32 * i + 8 * g + 4 * half) =
             f32x4{w.o[i][4 * g] * vs, w.o[i][4 * g + 1] * vs, w.o[i][4 * g + 2] * vs, w.o[i][4 * g + 3] * vs};
-    if (half == 0) a.parts.ml[slot] = f32x4{w.m, l, exact, 0.0f};
+    if (half == 0) a.parts.ml[slot] = f32x4{w.m, l, exact, more};
   }
 }
 
@@ -501,8 +503,9 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     // 2^66 of the queries (F16's become zeros: their scores are below 2^-20).
     const float smaller = S == BIASED && sc < 0x1p-60f ? 0x1p-66f : 1.0f;
     sc /= smaller;
-    w.slope = (S == BIASED || caps_first(S)) && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f;
-    if (S == BIASED) w.slope /= sc;
+    const Bias bias((S == BIASED || caps_first(S)) && a.slopes && has_row ? a.slopes[head] * LOG2E : 0.0f, first + tok, w.lo);
+    w.from = bias.from;
+    w.slope = S == BIASED ? bias.slope / sc : bias.slope;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       w.q[s] = u32x4{0, 0, 0, 0};
@@ -683,7 +686,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     };
     const float l = halves(w.l.get()), exact = LSE ? halves(w.exact) : 0.0f;
     const float vs = KV8 && a.cache.v_scale ? a.cache.v_scale[kvh] : 1.0f;
-    write_rows<T, LSE>(a, it, w, l, exact, kvh, wave, again(lane), vs);
+    write_rows<T, LSE>(a, it, w, l, exact, bias.more(first + tok), kvh, wave, again(lane), vs);
     if (kb0 < k1 && odd_piece == piece) {  // (the next piece's first barrier comes after all have read it)
 #pragma unroll 1
       for (int32_t key = k0; key < k1; ++key) {

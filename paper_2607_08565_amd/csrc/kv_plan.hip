@@ -263,13 +263,13 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
 constexpr int32_t JOIN_GRID = 2048;
 template <typename T, int D, bool FEW>
 __device__ __forceinline__ void write_row(const AttendArgs &a, const PlanSplit &s, int32_t in_req, int32_t kvh, int sub,
-                                          f32x4 acc, float m, float l, float exact) {
+                                          f32x4 acc, float m, float l, float exact, float more) {
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int64_t t = int64_t(s.tok0) + in_req / a.group;
   const int32_t head = kvh * a.group + in_req % a.group;
   *reinterpret_cast<u32x2 *>(a.out.data + t * a.out.token + head * a.out.head + sub * 4) =
       u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
-  if (a.lse && sub == 0) a.lse[t * a.n_q + head] = lse_of(m, exact, FEW ? T::FEW_SHIFT : T::MANY_SHIFT);
+  if (a.lse && sub == 0) a.lse[t * a.n_q + head] = lse_of(m, exact, FEW ? T::FEW_SHIFT : T::MANY_SHIFT, more);
 }
 template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
@@ -310,6 +310,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     const float ms = m == -INFINITY ? 0.0f : m;
     f32x4 acc{0, 0, 0, 0};
     float l = 0.0f, exact = 0.0f;
+    const float more = a.slopes ? ml->w : 0.0f;  // (the same in all parts)
     if (has) {
       const float w = exp2f(ml0.x - ms);
       l = w * ml0.y;
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
         }
       }
     }
-    if (!alone || side == 0) write_row<T, D, FEW>(a, s, in_req, kvh, sub, acc, m, l, exact);
+    if (!alone || side == 0) write_row<T, D, FEW>(a, s, in_req, kvh, sub, acc, m, l, exact, more);
     if (alone) __syncthreads();
   }
 }
