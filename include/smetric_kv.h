@@ -194,8 +194,10 @@ int smetric_attend(int32_t dtype, const smetric_kv_cache *cache /* host */, cons
  *   slopes  float32[n_q_heads], of either sign, magnitudes up to 2^20, or NULL: no bias
  * Scores are float32's: capped ones are off by some 2^-23 cap of caps up to 64, of larger ones by some
  * 2^-21 of themselves, a bias by (head_dim / 16 + 8) 2^-24 of how far it is below the largest that the
- * row sees.  Caps up to
- * 50.5 without slopes, BF16, chunks: weights are held times up to 2^62, so values up to 2^40 stay finite.
+ * row sees.
+ * Values' range: BF16 chunks with a cap up to 50.5 and no slopes have a fixed maximum in place of the
+ * running one, which values whose magnitude is 0 or in [2^-x, 2^x], x = 115 - 1.443 cap, bear: 2^42
+ * either way at 50, 2^71 at 30.  Smaller ones may become zeros there, larger ones infinite.
  * Host errors: smetric_attend's, and EINVAL for another cap. */
 typedef struct smetric_scores {
   float cap;

@@ -117,10 +117,11 @@ __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); 
 //   BIASED  the bias, divided by the factor to come, is where the products' sums begin, instead of 0 (each of
 //           head_dim / 16 products rounds it, but of the keys that count it is small: Bias)
 //   CAPPED  capped by so little that the weights need no running maximum, with BF16, whose weights have
-//           float32's range: scores are within cap of 0, and with m = min(cap, 84 - cap) in powers of
-//           two, cap up to 73 (50.5 natural), weights are between 2^-84 and 2^62: far from both ends
-//           also times values and summed over 2^24 keys.  That saves the maxima, a subtraction and the
-//           sums' scaling (2,048 tokens over 8,048: 195 us, without 175)
+//           float32's range: scores are within cap of 0 in powers of two, and with m = 11 weights are
+//           between 2^(-11 - cap) and 2^(cap - 11): times values between 2^(cap - 115) and 2^(115 - cap),
+//           summed over 2^24 keys, they stay between float32's ends, 2^-126 and 2^128.  Caps up to 73
+//           (50.5 natural) leave values 2^-42 to 2^42.  That saves the maxima, a subtraction and the sums'
+//           scaling (2,048 tokens over 8,048: 195 us, without 175)
 //   OTHER   capped and, maybe, biased then; FAR: caps above CAP_NEAR
 // Capping takes five instructions a score, two of them at half rate, as long as the matrix cores take
 // for it at heads of 128: so the first 32 keys' scores are capped during the other 32's products, and
@@ -128,8 +129,7 @@ __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); 
 enum Scores { PLAIN, BIASED, CAPPED, OTHER, FAR };
 constexpr bool caps(Scores s) { return s >= CAPPED; }
 constexpr bool caps_first(Scores s) { return s >= OTHER; }  // before a maximum is taken
-constexpr float CAPPED_MOST = 73.0f;
-__device__ __forceinline__ float capped_maximum(float cap) { return fminf(cap, 84.0f - cap); }
+constexpr float CAPPED_MOST = 73.0f, CAPPED_MAXIMUM = 11.0f;
 
 // The sum of the weights that the products with the values take, rounded as they are: a sum of unrounded
 // ones leaves equal values other than they are, by up to the weights' half step.  (lse has the unrounded
@@ -218,7 +218,7 @@ __device__ __forceinline__ float scores(const AttendArgs &a, const Rows<D, S> &w
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[j][r] = S == BIASED ? fmaf(w.slope, float(32 * j + 8 * (r / 4) + r % 4), from) : 0.0f;
-  const Capped cap(a, sc, S == CAPPED ? capped_maximum(a.cap_log2) : 0.0f);
+  const Capped cap(a, sc, S == CAPPED ? CAPPED_MAXIMUM : 0.0f);
   const auto capped = [&](float x) { return S == FAR ? cap.far(x) : cap(x); };
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -285,7 +285,7 @@ __device__ __forceinline__ void products(const AttendArgs &a, Rows<D, S> &w, con
   constexpr int DT = D / 32;
   constexpr bool CAP = S == CAPPED;
   const float base = exponent<T>(w);
-  const Capped capped(a, sc, CAP ? capped_maximum(a.cap_log2) : 0.0f);
+  const Capped capped(a, sc, CAP ? CAPPED_MAXIMUM : 0.0f);
   const int off = Values<D>::offset(again(lane));
   Values<D> v[2];
   u32x4 p[2];
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
     for (int i = 0; i < DT; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) w.o[i][r] = 0.0f;
-    w.m = S == CAPPED ? capped_maximum(a.cap_log2) : -INFINITY;
+    w.m = S == CAPPED ? CAPPED_MAXIMUM : -INFINITY;
     w.exact = 0.0f;
     const int32_t *table = a.cache.table + it.req * a.cache.table_stride;
 

@@ -241,7 +241,9 @@ def attend(q: torch.Tensor, cache: PagedCache, page_table: torch.Tensor, plan: P
     """smetric_attend: the new tokens' attention over the pages, as `plan` (made for the batch)
     splits it.  scale: 1 / sqrt(head_dim) by default; lse (float32 [tokens, heads]) is
     filled if given.  cap: scores become cap * tanh(score / cap); slopes (float32 [heads]): they get a
-    bias slopes[head] * (key's place - token's place) (smetric_attend_scores).  Returns out
+    bias slopes[head] * (key's place - token's place) (smetric_attend_scores).  With bfloat16 and a cap up
+    to 50.5, without slopes, values in the cache have to be 0 or between 2^-x and 2^x in magnitude, x =
+    115 - 1.443 cap (2^42 at a cap of 50): others may count as 0 or infinite.  Returns out
     [tokens, heads, head_dim]."""
     if plan.kv_len is None:
         raise ValueError("plan: make() it for the batch first")
