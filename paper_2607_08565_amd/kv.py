@@ -30,9 +30,12 @@ GROUP = 32  # components of a 4-bit cache with one exponent
 
 
 class _Kept:
-    """What the library is given by address: the last few of them stay, so that the address of one
-    that was made for a single call is good for that call."""
+    """Structures that callers of the library's entry points pass by address, also of one that was
+    made for that call alone: C.addressof(_Cache(...)).  ctypes would free it before the call, so the
+    last 64 stay, each with the structures that it points to (held).  The calls of this module hold
+    theirs themselves."""
     _last: collections.deque = collections.deque(maxlen=64)
+    held: tuple = ()
 
     def __init__(self, *fields, **named):
         super().__init__(*fields, **named)
@@ -108,7 +111,7 @@ class PagedCache:
                         _opt(v_scale, torch.float32, "v_scale"))
         if per == 2:
             self.exps = _Exps(k_exp.data_ptr(), v_exp.data_ptr(), strides(k_exp, 1), strides(v_exp, 1))
-            self.c.exps = C.addressof(self.exps)
+            self.c.exps, self.c.held = C.addressof(self.exps), (self.exps,)
         self.device = _device(k, v, k_scale, v_scale, k_exp, v_exp)
         self.ref = C.addressof(self.c)
 
