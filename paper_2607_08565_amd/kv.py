@@ -7,8 +7,9 @@ model's layer on a batch of requests, each with one new token or a chunk of them
     q = kv.append(cache, table, q_off, kv_len, k, v, q=q, rotary=rotary)  # per layer
     out = kv.attend(q, cache, table, plan)
 
-and, for an instance that hands a request's tokens on, kv.read of what the pages hold.  Tensors go in by data pointer on torch's current stream of the current device, which has to be
-theirs; there is no CPU fallback.
+and, for an instance that hands a request's tokens on, kv.read of what the pages hold.  Tensors go
+in by data pointer on torch's current stream of the current device, which has to be theirs; there is
+no CPU fallback.
 """
 from __future__ import annotations
 
@@ -24,8 +25,9 @@ try:
 except ImportError as e:
     raise RuntimeError("_kv_calls.so is missing or does not fit: build it first (__graft_entry__.build())") from e
 
-_E2M1, _E8M0 = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu  # two components a byte; a group's exponent
-_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2, _E2M1: 3}
+# two components a byte; a group's exponent (None where torch has no such type: no 4-bit caches then)
+_E2M1, _E8M0 = getattr(torch, "float4_e2m1fn_x2", None), getattr(torch, "float8_e8m0fnu", None)
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2, **({} if _E2M1 is None else {_E2M1: 3})}
 GROUP = 32  # components of a 4-bit cache with one exponent
 
 
@@ -119,7 +121,7 @@ class PagedCache:
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 16,
               dtype: torch.dtype = torch.bfloat16, device="cuda", **scales) -> "PagedCache":
         shape = (n_pages, n_kv_heads, page_size, head_dim)
-        if dtype == _E2M1:
+        if _E2M1 is not None and dtype == _E2M1:
             # a page's two exponents of a head beside each other: at heads of 128 and pages of 16 one line of memory
             e = torch.empty((n_pages, n_kv_heads, 2, page_size, head_dim // GROUP), dtype=_E8M0, device=device)
             shape = (*shape[:3], head_dim // 2)
