@@ -5,6 +5,8 @@ import sys
 SCRIPT = """
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
+with FakeTensorMode():  # (what torch itself imports for its stand-ins asks for the types)
+    torch.empty(2, device="cuda:0").data_ptr(), torch.empty((2, 2), device="cuda:0")[:, 0].stride()
 for name in ("float4_e2m1fn_x2", "float8_e8m0fnu"):
     delattr(torch, name)
 from paper_2607_08565_amd import kv
