@@ -1,4 +1,4 @@
-// Internal definitions shared by the paged-cache kernels: 16- and 8-bit floats, page
+// Internal definitions shared by the paged-cache kernels: 16-, 8- and 4-bit floats, page
 // addressing, and the plan of an attention step.  Not part of the ABI.
 #pragma once
 

@@ -435,9 +435,14 @@ __device__ __forceinline__ void add_not_finite(const AttendArgs &a, const PlanIt
   }
 }
 
+// Wavefronts a SIMD at least: heads of 64 leave registers for three, though a few values less than the compiler
+// takes by itself with the two sums of weights (24 mixed requests over 4-bit pages with lse 114 us, so 109; 4
+// chunks of 2,048 over 8-bit pages 275 without it, so 265).
+constexpr int wavefronts(int head_dim) { return head_dim == 64 ? 3 : at_once(head_dim); }
+
 // WIDE: page_size is a multiple of 16, so 16 aligned keys are neighbours in one page.  LSE: it is asked for.
 template <typename T, Pages KV, int D, bool WIDE, Scores S, bool LSE>
-__global__ __launch_bounds__(MT, at_once(D)) void many_kernel(AttendArgs a) {
+__global__ __launch_bounds__(MT, wavefronts(D)) void many_kernel(AttendArgs a) {
   constexpr bool KV8 = KV == PAGES8, KV4 = KV == PAGES4;
   constexpr int PB = KV4 ? piece4(D) : 16;  // bytes of a lane's load
   constexpr int LPR = page_bytes(KV, D) / PB;  // lanes per row of keys or values

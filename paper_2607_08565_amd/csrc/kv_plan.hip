@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     const float ms = m == -INFINITY ? 0.0f : m;
     f32x4 acc{0, 0, 0, 0};
     float l = 0.0f, exact = 0.0f;
-    const float more = a.slopes ? ml->w : 0.0f;  // (the same in all parts)
+    float more = ml0.w;  // (the same in all parts)
     if (has) {
       const float w = exp2f(ml0.x - ms);
       l = w * ml0.y;
@@ -324,6 +324,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
       const float w = exp2f(x.x - ms);
       l = fmaf(w, x.y, l);
       exact = fmaf(w, x.z, exact);
+      more = x.w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] = fmaf(w, v[i], acc[i]);
     }

@@ -3,7 +3,8 @@
 // Mathematics: a stored x stands for itself (16 bits), for x scale (E4M3, a scale per head) or for
 // x 2^(e - 127) (E2M1, an exponent per 32 components): widened in float32, rounded once.
 // Bound: memory, each row read once and written once as 16 bits; 8 components, 16 bytes, a lane, stored
-// past the caches (24 sessions of 8-bit pages 132 us, so 121).
+// past the caches (24 sessions of 8-bit pages 132 us, so 121; a few tokens that the next kernel reads pay little
+// for it: 4,096 read back and added up 16.9 us, 16.2 through the caches, one token 4.8 both).
 //
 // Measured: a session of 16,384 tokens, 4 heads of 128 in 4 bits (42 MB moved) 9.2 us, 4.6 TB/s; 24
 // sessions, 16 heads of 64 of 8 bits (630 MB) 117 us, 5.4 TB/s; 16 of 8,192, 8 heads of 128 of 16 bits
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(ET) void read_kernel(ReadArgs a) {
     for (int u = 0; u < EU; ++u, to += a.out[s].token) {
       if (t0 + u >= a.n_tokens) break;
       const u32x4 y = widened<T, KV>(x[u][s], e[u][s], scale[s]);
-      // past the caches: what is read back is more than they hold
+      // past the caches, see above
       __builtin_nontemporal_store(ok[u] ? y : u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4 *>(to));
     }
   }
