@@ -16,14 +16,14 @@
 // to the activations' type for it, as the matrix cores take 16-bit operands, and the output is divided by the sum
 // of rounded ones, so that equal values come out as they are; lse has the sum of unrounded ones.
 //
-// Measured: 32 requests decoding over 1.73 GB of cache 305 us, 5.7 TB/s (a copy of 4 GiB moves
-// 4.8); 64 drafted tokens over 0.58 GB 117 us; 131,072 keys of 8 bits (134 MB) 31 to 35 us, 24
-// of them here and the rest the joining; a lone token over 1,025 keys 9.4 us, two launches.
+// Measured: 32 requests decoding over 1.73 GB of cache 302 us, 5.7 TB/s (a copy of 4 GiB moves
+// 4.8); 64 drafted tokens over 0.58 GB 115 us; 131,072 keys of 8 bits (134 MB) 37 us, 24
+// of them here and the rest the joining; a lone token over 1,025 keys 9.6 us, two launches.
 // 4 bits, where a lane's 16 bytes are a group of 32 components, widened two at an instruction with its
-// exponent: the 32 requests (0.41 GB) 85 us, 4.8 TB/s, of which the kernel has 79, 5.2 TB/s; a lone
-// token 8.8; 131,072 keys 24; 32 requests over 16,384 at heads of 64 70, over 8,192 at heads of 256, one
+// exponent: the 32 requests (0.41 GB) 86 us, 4.8 TB/s, of which the kernel has 79, 5.2 TB/s; a lone
+// token 9.0; 131,072 keys 24.7; 32 requests over 16,384 at heads of 64 71, over 8,192 at heads of 256, one
 // wavefront a SIMD, 80.  Scores that are capped take 4 instructions more, two of them at half
-// rate: at heads of 256 16 requests decoding over 1.33 GB 233 us, 5.7 TB/s; over the 4-bit pages of 32 99.
+// rate: at heads of 256 16 requests decoding over 1.33 GB 233 us, 5.7 TB/s; over the 4-bit pages of 32 101.
 #include <math.h>
 
 #include "kv_attend.h"

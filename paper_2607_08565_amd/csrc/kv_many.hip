@@ -15,19 +15,19 @@
 // Weights are rounded to the activations' type for it, as the matrix cores take 16-bit operands, and
 // so are those that they are divided by the sum of (WeightSum); lse has the sum of unrounded ones.
 //
-// Measured: 4,096 tokens over 16,384 (32 heads of 128) 923 to 986 us, 1,041 to 976 TFLOP/s, from card to card; on the
-// faster one the library's product of matrices of 16,384 reaches 1,402, of 8,192 1,173.  The matrix cores work half of the cycles
-// and the vector instructions about as long (33 exponentials, 32 sums, 31 products and 16
-// maxima a step of 32 matrix instructions), on two wavefronts that overlap them in part, at a
+// Measured: 4,096 tokens over 16,384 (32 heads of 128) 919 to 953 us, 1,046 to 1,008 TFLOP/s, from card to card, with
+// lse 942 to 990; the library's product of matrices of 16,384 reaches 1,330 to 1,400, of 8,192 1,170 to 1,270.  The matrix
+// cores work half of the cycles and the vector instructions about as long (33 exponentials, 31 products,
+// 16 maxima and, with lse, 32 sums a step of 40 matrix instructions), on two wavefronts that overlap them in part, at a
 // clock that falls under the load (1.9 GHz).  With the keys always in the nearest cache it takes
 // 5 % less, without the exponentials 8 %, without the maximum 5 %.  Heads of 64 do half the
-// products for the same weights: 24 requests with up to 1,000 new tokens 108 to 112 us, 370 to 383 TFLOP/s.
+// products for the same weights: 24 requests with up to 1,000 new tokens, with lse, 116 us, 357 TFLOP/s.
 //
 // 8- and 4-bit keys and values are widened on the way to LDS, 4-bit ones two at an instruction with their
-// group's exponent, once for the 128 rows: over 4-bit pages the same 4,096 tokens take 916 to 954 us, and 2
-// chunks of 2,048 at heads of 256 309.  Scores that are capped or biased: enum Scores.  Capped, BF16,
-// 4,096 over 16,384: 1,061 to 1,110 us, F16 1,180 to 1,224; biased 989 to 1,035; 2,048 over 8,048 with a
-// window of 4,096 capped 167 to 175.
+// group's exponent, once for the 128 rows: over 4-bit pages the same 4,096 tokens take 915 to 941 us, with lse 943
+// to 1,005, and 2 chunks of 2,048 at heads of 256 304, 315.  Scores that are capped or biased: enum Scores.  Capped,
+// BF16, 4,096 over 16,384: 1,081 to 1,104 us, with lse 1,123 to 1,193; F16 1,183 to 1,204, 1,232 to 1,291; biased 995 to
+// 1,031, 1,031 to 1,087; 2,048 over 8,048 with a window of 4,096 capped 168 to 177, 173 to 187.
 #include <math.h>
 
 #include <type_traits>
@@ -135,8 +135,8 @@ constexpr float CAPPED_MOST = 73.0f, CAPPED_MAXIMUM = 11.0f;
 // ones leaves equal values other than they are, by up to the weights' half step.  (lse has the unrounded
 // ones' sum, 32 additions a step more.)  16 dot products with ones a step, each at half rate, or eight
 // matrix products of 8 cycles with a matrix of ones (4 x 4 x 4: a lane's own four), MATRIX: 4,096 tokens
-// over 16,384 with lse 1,005 us, with dot products 1,029, with a sum of unrounded ones 980; capped, whose
-// matrix cores wait less, 1,186 and 1,178; heads of 256, where registers are short, 309 and 298.
+// over 16,384 of 4 bits with lse 1,005 us, with dot products 1,029, with a sum of unrounded ones 980; capped
+// over BF16 pages 1,186 and 1,178; 2 chunks at heads of 256, where registers are short, 309 and 298.
 template <int D, Scores S>
 struct WeightSum {
   static constexpr bool MATRIX = D < 256 && !caps(S);
@@ -167,7 +167,7 @@ struct Rows {
   u32x4 q[D / 16];
   f32x16 o[D / 32];  // O^T: components 32 i + 8 (r / 4) + 4 half + r % 4
   float m;           // maximum
-  WeightSum<D, S> l; // of the half's keys: weights as the products take them, rounded
+  WeightSum<D, S> l;  // of the half's keys: weights as the products take them, rounded
   float exact;       // the same unrounded (LSE)
   int32_t hi, lo;    // the keys [lo, hi) that the row sees
   float slope;       // other scores: a key's bias by distance, of the products' sums or in powers of two

@@ -256,8 +256,8 @@ __global__ __launch_bounds__(PT) void plan_kernel(PlanArgs a) {
 }
 
 // Joins the parts of a cut tile: out = sum_p 2^(m_p - m) acc_p / sum_p 2^(m_p - m) l_p, in the
-// order of the parts, l_p the sums of rounded weights (PartView); lse takes those of unrounded ones.  D / 4 threads hold a row.  Tiles of many rows: the workgroup takes as
-// many rows at once (each of a few parts).  Tiles of few rows, which may have hundreds of
+// order of the parts, l_p the sums of rounded weights (PartView); lse takes those of unrounded ones.
+// D / 4 threads hold a row.  Tiles of many rows: the workgroup takes as many rows at once (each of a few parts).  Tiles of few rows, which may have hundreds of
 // parts, and of many where a few long requests share all of the parts: it takes one row's parts
 // side by side (2 requests of 7 new tokens over 47,760, 14 heads on 2: 44 us, so 7).
 constexpr int32_t JOIN_GRID = 2048;

@@ -15,8 +15,8 @@
 // Measured: 8,191 tokens of 40 heads of 128 29.5 us, 5.8 TB/s (a copy of 4 GiB moves 4.8); the
 // keys, values and queries of 6,249 tokens appended 32.4 us, 4.8 TB/s (pages in any order, the
 // queries kept in the caches for the attention); keys and values of 8 heads alone into 4-bit pages
-// 13 to 14 us, where instructions and the chain to the pages are what is left (32 MB are 7 us); a
-// token's append 4.4 us, its launch; of 256 5.2.
+// 13 to 15 us, where three dependent passes through LDS and the chain to the pages are what is left
+// (vector instructions 30 % of the cycles; 32 MB are 7 us); a token's append 4.5 us, its launch; of 256 5.2.
 #include "common.h"
 #include "kv_common.h"
 
